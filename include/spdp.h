@@ -304,6 +304,184 @@ int spdp_hellinger_noalloc(spdp_state *s, const double *p, int32_t kp, const dou
 int spdp_align_topics(const double *h, int32_t kp, int32_t kq, int32_t *match, double *total);
 
 /*
+ * Words that a model answers with.  From the point estimates a document's word
+ * probabilities are p(w | d) = sum_k theta[d][k] phi[w][k]: a score for every
+ * word of the vocabulary, from which words are suggested (the best ones, those
+ * the document has made less likely or ruled out) or drawn (posterior
+ * predictive checks).  The entry points below are the steps, and spdp_predict
+ * runs them in one call.  They use the state's device and stream only (the
+ * state's counts are neither read nor changed), take device pointers only, allocate
+ * nothing and do not synchronise: they can be captured into a HIP graph.
+ * Buffers are checked to be device memory that holds their size (against the
+ * device allocation, not against a caller's sub-range of it); what they hold
+ * is not checked on the host, and each entry point says what becomes of values
+ * out of range.  A workspace belongs to one call at a time: calls that overlap
+ * (other streams, other graphs) need workspaces of their own.
+ */
+
+/* Types of values in device memory. */
+#define SPDP_F64 0
+#define SPDP_F32 1
+#define SPDP_F16 2
+#define SPDP_BF16 3
+
+#define SPDP_BLOCK8 128   /* columns that share a scale in spdp_rows8             */
+#define SPDP_MAX_TAKE 256 /* most words that spdp_top takes from a row            */
+
+/*
+ * Rows in 8-bit floating point (e4m3: largest value 448, no infinities), with a
+ * power of two as the scale of each block of SPDP_BLOCK8 columns of a row:
+ * element (i, k) is q[i][k] 2^(e[i][k / SPDP_BLOCK8] - 127).
+ */
+typedef struct {
+    int64_t rows;               /* 0 <= rows < 2^31                                   */
+    int32_t cols;               /* 1 <= cols < 2^24; blocks = ceil(cols / SPDP_BLOCK8) */
+    uint8_t *q;                 /* device [rows][blocks SPDP_BLOCK8], 16-byte aligned; the
+                                   columns behind cols hold 0                          */
+    uint8_t *e;                 /* device [rows][blocks], values 0 .. 254              */
+} spdp_rows8;
+
+/*
+ * Round rows x [out->rows][out->cols] (device, SPDP_F64 or SPDP_F32, ld elements
+ * from one row to the next) to 8 bits.  A block's scale is 2^e with the least e
+ * in [-127, 127] for which its largest finite magnitude is at most 448 2^e (-127
+ * for a block of zeros); x 2^-e is rounded once, to nearest even.  A value that is
+ * not finite, or beyond 448 2^127, becomes NaN and leaves the scale to the others.
+ * Theta and phi as spdp_estimates writes them are such rows (topics contiguous).
+ * Errors: E_ARG (NULL pointer, size out of range, ld < cols, another type, q not
+ * aligned, a buffer that is not device memory or too short), E_HIP.
+ */
+int spdp_pack8(spdp_state *s, const void *x, int32_t type, int64_t ld, const spdp_rows8 *out);
+
+/*
+ * c[i][j] = sum_k a[i][k] b[j][k] of rows in 8 bits with the same columns, the
+ * elements exact (bf16, which holds them for scales of 2^-124 to 2^119; beyond, they
+ * round to bf16 or become infinite) and sums in fp32, or its natural logarithm if log_scores != 0 (-inf where the sum is 0, NaN
+ * where it is negative), rounded to `type` (SPDP_F32, SPDP_F16 or SPDP_BF16).  c is
+ * device [a->rows][b->rows] with ld elements from one row to the next; elements
+ * behind a row's end are left as they are.
+ * Errors: E_ARG (NULL pointer, sizes out of range or columns that differ, ld <
+ * b->rows, another type, buffers as for spdp_pack8), E_RANGE (more than 2^31 tiles
+ * of 16 x 16 outputs), E_HIP.
+ */
+int spdp_product8(spdp_state *s, const spdp_rows8 *a, const spdp_rows8 *b, int32_t log_scores,
+                  void *c, int32_t type, int64_t ld);
+
+/*
+ * Rules on the scores of `rows` documents over n_words words.  Score x of word w
+ * becomes, each step rounded to fp32,
+ *   x1  = c > 0 ? (x > 0 ? x / repeat : x * repeat) : x
+ *   x2  = c > 0 ? x1 - (presence + frequency * c) : x1
+ *   x3  = x2 + bias[w]
+ *   x'  = word w is allowed ? x3 : -inf  (whatever x3 is, NaN included)
+ * with c the number of times that w is among the document's listed words and
+ * penalties[row] = {repeat, presence, frequency} ({1, 0, 0} changes nothing).
+ * Bias rows and masks are tables from which a row takes one, by its group or by
+ * the state of a grammar.  Parts that are NULL are left out.
+ */
+typedef struct {
+    int64_t rows;               /* documents                                          */
+    int32_t n_words;            /* words of the vocabulary                            */
+    int32_t n_bias;             /* bias rows                                          */
+    int32_t n_masks;            /* masks                                              */
+    int64_t n_listed;           /* entries of words                                   */
+    const int64_t *doc_off;     /* device [rows + 1]: row i lists words[doc_off[i] ..
+                                   doc_off[i + 1]) in any order, repeated as often as they
+                                   count; clamped to [0, n_listed], empty if decreasing  */
+    const int32_t *words;       /* device [n_listed]; those outside [0, n_words) are
+                                   ignored                                            */
+    const float *penalties;     /* device [rows][3]; with doc_off                     */
+    const float *bias;          /* device [n_bias][n_words]                           */
+    const int32_t *bias_of;     /* device [rows]: bias row of each row, negative for none;
+                                   NULL: row 0 for all                                */
+    const uint32_t *mask;       /* device [n_masks][ceil(n_words / 32)]: word w is allowed
+                                   if bit w % 32 of word w / 32 is set                */
+    const int32_t *mask_of;     /* device [rows]: as bias_of (negative: all allowed)  */
+} spdp_rules;                   /* (an index past its table makes the row's x' NaN)   */
+
+/*
+ * y = x' : scores x under the rules (device [rows][n_words], ldx and ldy elements
+ * from one row to the next, both of `type` SPDP_F32, SPDP_F16 or SPDP_BF16).  y may be x with
+ * ldy = ldx; other overlaps are an error.  Elements behind a row's end are left as
+ * they are.
+ * Errors: E_ARG (NULL pointer, sizes out of range, rules of another size or
+ * incomplete, another type, overlapping buffers, buffers as for spdp_pack8),
+ * E_RANGE (more than 2^31 chunks of 4096 scores), E_HIP.
+ */
+int spdp_adjust(spdp_state *s, const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
+                const spdp_rules *rules);
+
+/* Bytes of workspace that spdp_top (take = k) and spdp_draw need for their sizes. */
+int spdp_words_work(int64_t rows, int32_t n_words, int32_t take, int64_t *bytes);
+
+/*
+ * The k best words of every row of scores x (device [rows][n_words], as for
+ * spdp_adjust), under the rules if `rules` is not NULL: word [rows][k] int32 and
+ * their scores value [rows][k] fp32 (device), best first, ties to the lowest
+ * word.  Scores that are -inf or NaN are never taken; places that are left hold
+ * word -1 and value -inf.  work: device, 16-byte aligned.
+ * Errors: E_ARG (as spdp_adjust; k outside [1, SPDP_MAX_TAKE]; a workspace that is
+ * too small or not aligned), E_RANGE, E_HIP.
+ */
+int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
+             int32_t n_words, const spdp_rules *rules, int32_t k, int32_t *word, float *value,
+             void *work, int64_t work_bytes);
+
+/*
+ * `draws` words of every row, drawn independently from the law with weights exp((x'
+ * - max x') / temperature): the first word whose prefix sum of the weights exceeds
+ * u times their sum, in fp64.  word [rows][draws] int32 and logp [rows][draws]
+ * fp32, the logarithm of the drawn word's probability (device).  u is device
+ * [rows][draws] fp64 (0 and less draw the first word with positive weight; 1 and
+ * more, and NaN, the last); NULL takes the uniforms x0 2^-32 of Philox4x32-10
+ * keyed by `seed` at counter (row draws + draw, step) with purpose 4 (first word).
+ * A row without a law (every score -inf; NaN or +inf among them) gives word -1 and
+ * logp NaN.
+ * Errors: E_ARG (as spdp_top; draws outside [0, 2^20], temperature outside [1e-6, 1e6]),
+ * E_RANGE, E_HIP.
+ */
+int spdp_draw(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
+              int32_t n_words, const spdp_rules *rules, double temperature, int32_t draws,
+              const double *u, uint64_t seed, uint32_t step, int32_t *word, float *logp,
+              void *work, int64_t work_bytes);
+
+/*
+ * Words for documents: log p(w | d) from docs (theta, one row per document) and
+ * words (phi, one row per word), under the rules (may be NULL), and of them any of
+ *   scores     the scores x' themselves (device [docs->rows][words->rows], ld, type)
+ *   top_word,  the k best words and their scores (as spdp_top; k = 0: none)
+ *   top_value
+ *   draw_word, `draws` words drawn and their log probabilities (as spdp_draw; draws
+ *   draw_logp  = 0: none)
+ * Without `scores` they are held in the workspace in `type`, as many documents at a
+ * time as it has room for; the rules are then applied to them in fp32 as they are
+ * read, while with `scores` the words are chosen from the scores as stored (the same
+ * thing for SPDP_F32).  spdp_predict_work gives the bytes for a good number of
+ * documents at a time; any that hold one document will do.
+ * Errors: as the steps; E_ARG for a workspace too small for one document.
+ */
+typedef struct {
+    void *scores;               /* or NULL                                            */
+    int64_t ld;                 /* elements from one row of scores to the next        */
+    int32_t type;               /* of the scores                                      */
+    int32_t k;
+    int32_t *top_word;
+    float *top_value;
+    int32_t draws;
+    double temperature;
+    const double *u;
+    uint64_t seed;
+    uint32_t step;
+    int32_t *draw_word;
+    float *draw_logp;
+} spdp_answer;
+
+int spdp_predict_work(int64_t docs, int32_t n_words, int32_t type, int32_t k, int64_t *bytes);
+int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
+                 const spdp_rules *rules, const spdp_answer *answer, void *work,
+                 int64_t work_bytes);
+
+/*
  * Checkpoint: export z [N] int32 and r [N] uint8 (either may be NULL).
  * Synchronises.  Errors: E_ARG, E_HIP.
  */

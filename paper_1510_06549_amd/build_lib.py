@@ -18,6 +18,8 @@ SOURCES = ["api.hip", "setup.hip", "counts.hip", "sample.hip", "sample_assoc.hip
            "loglik.hip",
            "estimate.hip",
            "hellinger.hip",
+           "rows8.hip",
+           "words.hip",
            "probe.hip",
            "check.hip"]
 LIB = os.path.join(HERE, "libspdp.so")

@@ -1027,6 +1027,371 @@ int spdp_align_topics(const double *h, int32_t kp, int32_t kq, int32_t *match, d
     return SPDP_OK;
 }
 
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Words of documents
+// ---------------------------------------------------------------------------
+namespace {
+
+#define CALL(expr)                         \
+    do {                                   \
+        const int rc_ = (expr);            \
+        if (rc_ != SPDP_OK) return rc_;    \
+    } while (0)
+
+// Makes a device current and the caller's current again.
+class OnDevice {
+public:
+    explicit OnDevice(int device)
+    {
+        if ((err_ = hipGetDevice(&before_)) == hipSuccess && before_ != device)
+            if ((err_ = hipSetDevice(device)) == hipSuccess) back_ = true;
+    }
+    ~OnDevice()
+    {
+        if (back_) (void)hipSetDevice(before_);
+    }
+    hipError_t error() const { return err_; }
+
+private:
+    int before_ = 0;
+    bool back_ = false;
+    hipError_t err_;
+};
+
+// That [p, p + bytes) lies in one device allocation.
+int check_device(const void *p, int64_t bytes, const char *name)
+{
+    if (bytes == 0) return SPDP_OK;
+    if (!p) return fail(SPDP_E_ARG, "%s is NULL", name);
+    hipDeviceptr_t base = nullptr;
+    size_t size = 0;
+    if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(SPDP_E_ARG, "%s is not device memory", name);
+    }
+    const int64_t at = static_cast<const char *>(p) - static_cast<const char *>(base);
+    if (bytes > (int64_t)size - at)
+        return fail(SPDP_E_ARG, "%s: %lld bytes run past its allocation", name, (long long)bytes);
+    return SPDP_OK;
+}
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+int64_t type_size(int32_t type)
+{
+    return type == SPDP_F64 ? 8 : type == SPDP_F32 ? 4 : 2;
+}
+
+// The bytes of rows of n elements, ld elements from one row to the next.
+int matrix_bytes(int64_t rows, int64_t n, int64_t ld, int32_t type, const char *name,
+                 int64_t *bytes)
+{
+    if (ld < n) return fail(SPDP_E_ARG, "%s: rows of %lld elements overlap at ld = %lld", name,
+                            (long long)n, (long long)ld);
+    *bytes = 0;
+    if (rows == 0) return SPDP_OK;
+    int64_t last = 0;
+    if (__builtin_mul_overflow(rows - 1, ld, &last) || last > (INT64_MAX >> 4) - n)
+        return fail(SPDP_E_ARG, "%s: more elements than memory holds", name);
+    *bytes = (last + n) * type_size(type);
+    return SPDP_OK;
+}
+
+// Rows of scores: their type, sizes and buffer.
+int check_scores(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t n,
+                 const char *name)
+{
+    if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
+        return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+    if (rows < 0 || rows > INT32_MAX || n < 1 || n > INT32_MAX)
+        return fail(SPDP_E_ARG, "need 0 <= rows < 2^31 and 1 <= n_words < 2^31");
+    int64_t bytes = 0;
+    CALL(matrix_bytes(rows, n, ld, type, name, &bytes));
+    if ((uintptr_t)x % type_size(type) != 0) return fail(SPDP_E_ARG, "%s is misaligned", name);
+    return check_device(x, bytes, name);
+}
+
+int check_rows8(const spdp_rows8 *a, const char *name)
+{
+    if (!a) return fail(SPDP_E_ARG, "%s is NULL", name);
+    if (a->rows < 0 || a->rows > INT32_MAX || a->cols < 1 || a->cols >= 1 << 24)
+        return fail(SPDP_E_ARG, "%s: need 0 <= rows < 2^31 and 1 <= cols < 2^24", name);
+    if (!aligned16(a->q)) return fail(SPDP_E_ARG, "%s: q is not 16-byte aligned", name);
+    const int64_t blocks = a->rows * blocks8(a->cols);
+    CALL(check_device(a->q, blocks * kBlock8, name));
+    return check_device(a->e, blocks, name);
+}
+
+int check_rules(const spdp_rules *r, int64_t rows, int64_t n)
+{
+    if (r->rows != rows || r->n_words != n)
+        return fail(SPDP_E_ARG, "rules for %lld x %d scores, not %lld x %lld", (long long)r->rows,
+                    r->n_words, (long long)rows, (long long)n);
+    if (r->n_bias < 0 || r->n_masks < 0 || r->n_listed < 0 || r->n_listed > INT64_MAX >> 4)
+        return fail(SPDP_E_ARG, "rules: negative size");
+    if (rows == 0) return SPDP_OK;
+    if (r->doc_off) {
+        if (!r->penalties) return fail(SPDP_E_ARG, "rules: listed words without penalties");
+        CALL(check_device(r->doc_off, (rows + 1) * 8, "rules: doc_off"));
+        CALL(check_device(r->words, r->n_listed * 4, "rules: words"));
+        CALL(check_device(r->penalties, rows * 12, "rules: penalties"));
+    } else if (r->words || r->penalties) {
+        return fail(SPDP_E_ARG, "rules: words and penalties need doc_off");
+    }
+    const struct {
+        const void *table;
+        const int32_t *of;
+        int64_t entries, width;
+        const char *name, *name_of;
+    } tables[2] = {{r->bias, r->bias_of, r->n_bias, n, "rules: bias", "rules: bias_of"},
+                   {r->mask, r->mask_of, r->n_masks, (n + 31) / 32, "rules: mask",
+                    "rules: mask_of"}};
+    for (const auto &t : tables) {
+        if (!t.table) {
+            if (t.of) return fail(SPDP_E_ARG, "%s without its table", t.name_of);
+            continue;
+        }
+        if (t.entries < 1) return fail(SPDP_E_ARG, "%s has no rows", t.name);
+        CALL(check_device(t.table, t.entries * t.width * 4, t.name));
+        if (t.of) CALL(check_device(t.of, rows * 4, t.name_of));
+    }
+    return SPDP_OK;
+}
+
+int check_blocks(int64_t blocks)
+{
+    if (blocks > INT32_MAX)
+        return fail(SPDP_E_RANGE, "%lld workgroups exceed a launch", (long long)blocks);
+    return SPDP_OK;
+}
+
+int check_work(const void *work, int64_t have, int64_t need)
+{
+    if (have < need)
+        return fail(SPDP_E_ARG, "a workspace of %lld bytes, not %lld", (long long)need,
+                    (long long)have);
+    if (!aligned16(work)) return fail(SPDP_E_ARG, "the workspace is not 16-byte aligned");
+    return check_device(work, need, "work");
+}
+
+int check_take(int32_t k, int64_t rows, const int32_t *word, const float *value)
+{
+    if (k < 1 || k > SPDP_MAX_TAKE)
+        return fail(SPDP_E_ARG, "k must be in [1, %d]", SPDP_MAX_TAKE);
+    CALL(check_device(word, rows * k * 4, "word"));
+    return check_device(value, rows * k * 4, "value");
+}
+
+int check_draws(int32_t draws, double temperature, int64_t rows, const double *u,
+                const int32_t *word, const float *logp)
+{
+    if (draws < 0 || draws > 1 << 20) return fail(SPDP_E_ARG, "draws must be in [0, 2^20]");
+    if (!(temperature >= 1e-6 && temperature <= 1e6))
+        return fail(SPDP_E_ARG, "temperature must be in [1e-6, 1e6]");
+    if (u) CALL(check_device(u, rows * draws * 8, "u"));
+    CALL(check_device(word, rows * draws * 4, "word"));
+    return check_device(logp, rows * draws * 4, "logp");
+}
+
+// The rules of the rows from `row` on.
+spdp_rules rules_from(const spdp_rules &r, int64_t row)
+{
+    spdp_rules o = r;
+    if (o.doc_off) {
+        o.doc_off += row;
+        o.penalties += 3 * row;
+    }
+    if (o.bias_of) o.bias_of += row;
+    if (o.mask_of) o.mask_of += row;
+    return o;
+}
+
+// Workspace of spdp_predict for `rows` documents at a time: their scores (unless
+// the caller keeps them), then what choosing words needs.
+int64_t scores_room(int64_t rows, int64_t n, int32_t type, bool kept)
+{
+    return kept ? 0 : (rows * n * type_size(type) + 255) / 256 * 256;
+}
+
+}  // namespace
+
+extern "C" {
+
+int spdp_pack8(spdp_state *s, const void *x, int32_t type, int64_t ld, const spdp_rows8 *out)
+{
+    if (!s) return fail(SPDP_E_ARG, "state is NULL");
+    if (type != SPDP_F64 && type != SPDP_F32)
+        return fail(SPDP_E_ARG, "rows to pack are SPDP_F64 or SPDP_F32");
+    CALL(check_rows8(out, "out"));
+    int64_t bytes = 0;
+    CALL(matrix_bytes(out->rows, out->cols, ld, type, "x", &bytes));
+    if ((uintptr_t)x % type_size(type) != 0) return fail(SPDP_E_ARG, "x is misaligned");
+    CALL(check_device(x, bytes, "x"));
+    CALL(check_blocks(out->rows * blocks8(out->cols) / 4 + 1));
+    OnDevice on(s->device);
+    HIP_TRY(on.error());
+    HIP_TRY(launch_pack8(x, type, out->rows, out->cols, ld, out->q, out->e, s->st));
+    return SPDP_OK;
+}
+
+int spdp_product8(spdp_state *s, const spdp_rows8 *a, const spdp_rows8 *b, int32_t log_scores,
+                  void *c, int32_t type, int64_t ld)
+{
+    if (!s) return fail(SPDP_E_ARG, "state is NULL");
+    CALL(check_rows8(a, "a"));
+    CALL(check_rows8(b, "b"));
+    if (a->cols != b->cols)
+        return fail(SPDP_E_ARG, "rows of %d and %d columns", a->cols, b->cols);
+    if (b->rows == 0) return SPDP_OK;
+    CALL(check_scores(c, ld, type, a->rows, b->rows, "c"));
+    CALL(check_blocks((a->rows + 15) / 16 * ((b->rows + 15) / 16)));
+    OnDevice on(s->device);
+    HIP_TRY(on.error());
+    HIP_TRY(launch_product8(*a, *b, log_scores != 0, c, type, ld, s->st));
+    return SPDP_OK;
+}
+
+int spdp_adjust(spdp_state *s, const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
+                const spdp_rules *rules)
+{
+    if (!s) return fail(SPDP_E_ARG, "state is NULL");
+    if (!rules) return fail(SPDP_E_ARG, "rules is NULL");
+    const int64_t rows = rules->rows, n = rules->n_words;
+    CALL(check_scores(x, ldx, type, rows, n, "x"));
+    CALL(check_scores(y, ldy, type, rows, n, "y"));
+    CALL(check_rules(rules, rows, n));
+    if (rows > 0 && (x != y || ldx != ldy)) {
+        const int64_t size = type_size(type);
+        const uintptr_t x0 = (uintptr_t)x, x1 = x0 + ((rows - 1) * ldx + n) * size;
+        const uintptr_t y0 = (uintptr_t)y, y1 = y0 + ((rows - 1) * ldy + n) * size;
+        if (x0 < y1 && y0 < x1)
+            return fail(SPDP_E_ARG, "x and y overlap and are not the same rows");
+    }
+    CALL(check_blocks(words_blocks(rows, n)));
+    OnDevice on(s->device);
+    HIP_TRY(on.error());
+    HIP_TRY(launch_adjust(x, ldx, y, ldy, type, rows, n, *rules, s->st));
+    return SPDP_OK;
+}
+
+int spdp_words_work(int64_t rows, int32_t n_words, int32_t take, int64_t *bytes)
+{
+    if (!bytes) return fail(SPDP_E_ARG, "null argument");
+    if (rows < 0 || rows > INT32_MAX || n_words < 1 || take < 0)
+        return fail(SPDP_E_ARG, "size out of range");
+    *bytes = words_work(rows, n_words, take < SPDP_MAX_TAKE ? take : SPDP_MAX_TAKE);
+    return SPDP_OK;
+}
+
+int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
+             int32_t n_words, const spdp_rules *rules, int32_t k, int32_t *word, float *value,
+             void *work, int64_t work_bytes)
+{
+    if (!s) return fail(SPDP_E_ARG, "state is NULL");
+    CALL(check_scores(x, ld, type, rows, n_words, "x"));
+    if (rules) CALL(check_rules(rules, rows, n_words));
+    CALL(check_take(k, rows, word, value));
+    CALL(check_work(work, work_bytes, words_work(rows, n_words, k)));
+    CALL(check_blocks(words_blocks(rows, n_words)));
+    OnDevice on(s->device);
+    HIP_TRY(on.error());
+    HIP_TRY(launch_top(x, ld, type, rows, n_words, rules ? *rules : spdp_rules{}, k, word, value,
+                       work, s->st));
+    return SPDP_OK;
+}
+
+int spdp_draw(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
+              int32_t n_words, const spdp_rules *rules, double temperature, int32_t draws,
+              const double *u, uint64_t seed, uint32_t step, int32_t *word, float *logp,
+              void *work, int64_t work_bytes)
+{
+    if (!s) return fail(SPDP_E_ARG, "state is NULL");
+    CALL(check_scores(x, ld, type, rows, n_words, "x"));
+    if (rules) CALL(check_rules(rules, rows, n_words));
+    CALL(check_draws(draws, temperature, rows, u, word, logp));
+    CALL(check_work(work, work_bytes, words_work(rows, n_words, 0)));
+    CALL(check_blocks(words_blocks(rows, n_words)));
+    OnDevice on(s->device);
+    HIP_TRY(on.error());
+    HIP_TRY(launch_draw(x, ld, type, rows, n_words, rules ? *rules : spdp_rules{}, temperature,
+                        draws, u, seed, step, 0, word, logp, work, s->st));
+    return SPDP_OK;
+}
+
+int spdp_predict_work(int64_t docs, int32_t n_words, int32_t type, int32_t k, int64_t *bytes)
+{
+    if (!bytes) return fail(SPDP_E_ARG, "null argument");
+    if (docs < 0 || docs > INT32_MAX || n_words < 1 || k < 0 || k > SPDP_MAX_TAKE)
+        return fail(SPDP_E_ARG, "size out of range");
+    if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
+        return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+    int64_t rows = kPredictScores / (n_words * type_size(type));
+    rows = rows < 1 ? 1 : rows;
+    rows = rows < docs ? rows : docs;
+    *bytes = scores_room(rows, n_words, type, false) + words_work(rows, n_words, k);
+    return SPDP_OK;
+}
+
+int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
+                 const spdp_rules *rules, const spdp_answer *answer, void *work,
+                 int64_t work_bytes)
+{
+    if (!s || !answer) return fail(SPDP_E_ARG, "null argument");
+    CALL(check_rows8(docs, "docs"));
+    CALL(check_rows8(words, "words"));
+    if (docs->cols != words->cols)
+        return fail(SPDP_E_ARG, "rows of %d and %d columns", docs->cols, words->cols);
+    const spdp_answer a = *answer;
+    const int64_t D = docs->rows, V = words->rows;
+    if (V < 1) return fail(SPDP_E_ARG, "no words");
+    const bool kept = a.scores != nullptr;
+    if (kept) CALL(check_scores(a.scores, a.ld, a.type, D, V, "scores"));
+    else if (a.type != SPDP_F32 && a.type != SPDP_F16 && a.type != SPDP_BF16)
+        return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+    if (rules) CALL(check_rules(rules, D, V));
+    if (a.k != 0) CALL(check_take(a.k, D, a.top_word, a.top_value));
+    if (a.draws != 0) CALL(check_draws(a.draws, a.temperature, D, a.u, a.draw_word, a.draw_logp));
+    if (D == 0) return SPDP_OK;
+    const bool choose = a.k > 0 || a.draws > 0;
+    auto need = [&](int64_t rows) {
+        return scores_room(rows, V, a.type, kept) + (choose ? words_work(rows, V, a.k) : 0);
+    };
+    if (!kept && !choose) return SPDP_OK;  // nothing asked for
+    int64_t rows = D;  // documents at a time
+    while (rows > 1 && need(rows) > work_bytes) rows = (rows + 1) / 2;
+    CALL(check_work(work, work_bytes, need(rows)));
+    CALL(check_blocks(words_blocks(rows, V)));
+    CALL(check_blocks((rows + 15) / 16 * ((V + 15) / 16)));
+    OnDevice on(s->device);
+    HIP_TRY(on.error());
+    const int64_t blocks = blocks8(docs->cols);
+    for (int64_t d = 0; d < D; d += rows) {
+        const int64_t m = rows < D - d ? rows : D - d;
+        const spdp_rows8 part{m, docs->cols, docs->q + d * blocks * kBlock8, docs->e + d * blocks};
+        const int64_t ld = kept ? a.ld : V;
+        void *x = kept ? static_cast<char *>(a.scores) + d * ld * type_size(a.type) : work;
+        void *rest = static_cast<char *>(work) + scores_room(rows, V, a.type, kept);
+        HIP_TRY(launch_product8(part, *words, true, x, a.type, ld, s->st));
+        spdp_rules r{};
+        if (rules) r = rules_from(*rules, d);
+        if (rules && kept) {
+            HIP_TRY(launch_adjust(x, ld, x, ld, a.type, m, V, r, s->st));
+            r = spdp_rules{};
+        }
+        if (a.k > 0)
+            HIP_TRY(launch_top(x, ld, a.type, m, V, r, a.k, a.top_word + d * a.k,
+                               a.top_value + d * a.k, rest, s->st));
+        if (a.draws > 0)
+            HIP_TRY(launch_draw(x, ld, a.type, m, V, r, a.temperature, a.draws,
+                                a.u ? a.u + d * a.draws : nullptr, a.seed, a.step, d * a.draws,
+                                a.draw_word + d * a.draws, a.draw_logp + d * a.draws, rest,
+                                s->st));
+    }
+    return SPDP_OK;
+}
+
 int spdp_get_assignments(const spdp_state *s, int32_t *z, uint8_t *r, int where)
 {
     if (!s) return fail(SPDP_E_ARG, "state is NULL");

@@ -13,7 +13,7 @@ namespace spdp {
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC'11).  Counter (token lo, token
 // hi, sweep, purpose), key = seed.  Only word 0 of each block is used.
 // ---------------------------------------------------------------------------
-enum : uint32_t { kPurposeSample = 0u, kPurposeInit = 1u };
+enum : uint32_t { kPurposeSample = 0u, kPurposeInit = 1u, kPurposeWord = 4u };
 
 __host__ __device__ __forceinline__ uint32_t philox_x0(uint64_t seed, uint64_t ctr_lo64,
                                                        uint32_t c2, uint32_t c3)
@@ -351,6 +351,28 @@ hipError_t launch_hellinger(const HellingerPlan &p, const double *P, int32_t kp,
 // least-total-cost matching of the rows of c [kp][kq] (kp <= kq, finite):
 // match[i] = column of row i; returns the total cost (host code)
 double align_topics_host(const double *c, int32_t kp, int32_t kq, int32_t *match);
+
+// Words of documents (rows8.hip, words.hip).  Sizes and buffers are checked at the
+// boundary; rules hold null pointers for parts that are left out.
+constexpr int32_t kBlock8 = SPDP_BLOCK8;
+constexpr int64_t kPredictScores = 96 << 20;  // bytes of scores that spdp_predict holds at a time
+inline int32_t blocks8(int32_t cols) { return (cols + kBlock8 - 1) / kBlock8; }
+hipError_t launch_pack8(const void *x, int32_t type, int64_t rows, int32_t cols, int64_t ld,
+                        uint8_t *q, uint8_t *e, hipStream_t st);
+hipError_t launch_product8(const spdp_rows8 &a, const spdp_rows8 &b, bool log, void *c,
+                           int32_t type, int64_t ld, hipStream_t st);
+hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
+                         int64_t rows, int64_t V, const spdp_rules &rules, hipStream_t st);
+int64_t words_work(int64_t rows, int64_t V, int32_t take);  // bytes for either of the next two
+int64_t words_blocks(int64_t rows, int64_t V);              // workgroups of a launch
+hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
+                      const spdp_rules &rules, int32_t k, int32_t *word, float *value, void *work,
+                      hipStream_t st);
+// draw t of row i is draw number draw0 + i draws + t of the seed's stream
+hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
+                       const spdp_rules &rules, double temperature, int32_t draws,
+                       const double *u, uint64_t seed, uint32_t step, int64_t draw0,
+                       int32_t *word, float *logp, void *work, hipStream_t st);
 
 // The sampler's per-lane topic count for K topics (4 at most per dwordx4).
 hipError_t launch_read_probe(const void *buf, int64_t bytes, int32_t row_bytes, int64_t rows,

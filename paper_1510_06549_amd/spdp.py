@@ -24,6 +24,9 @@ SPDP_E_STATE = -5
 SPDP_MAX_K = 1024
 SPDP_MAX_SOURCES = 8
 SPDP_NKERNELS = 4
+SPDP_F64, SPDP_F32, SPDP_F16, SPDP_BF16 = 0, 1, 2, 3
+SPDP_BLOCK8 = 128
+SPDP_MAX_TAKE = 256
 KERNEL_CLASSES = ("sample", "rebuild", "base", "totals")
 
 # Every entry point of include/spdp.h, in declaration order.
@@ -35,6 +38,8 @@ EXPORTS = (
     "spdp_create_assoc", "spdp_get_slots", "spdp_set_assignments_assoc", "spdp_max_sources",
     "spdp_sweep_async", "spdp_read_probe", "spdp_check", "spdp_debug_poke",
     "spdp_hellinger_noalloc", "spdp_debug_weight_rows",
+    "spdp_pack8", "spdp_product8", "spdp_adjust", "spdp_words_work", "spdp_top", "spdp_draw",
+    "spdp_predict_work", "spdp_predict",
 )
 
 
@@ -66,6 +71,45 @@ class _Assoc(C.Structure):
         ("row_off", C.c_void_p),
         ("src", C.c_void_p),
         ("p", C.c_void_p),
+    ]
+
+
+class _Rows8(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("q", C.c_void_p), ("e", C.c_void_p)]
+
+
+class _Rules(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64),
+        ("n_words", C.c_int32),
+        ("n_bias", C.c_int32),
+        ("n_masks", C.c_int32),
+        ("n_listed", C.c_int64),
+        ("doc_off", C.c_void_p),
+        ("words", C.c_void_p),
+        ("penalties", C.c_void_p),
+        ("bias", C.c_void_p),
+        ("bias_of", C.c_void_p),
+        ("mask", C.c_void_p),
+        ("mask_of", C.c_void_p),
+    ]
+
+
+class _Answer(C.Structure):
+    _fields_ = [
+        ("scores", C.c_void_p),
+        ("ld", C.c_int64),
+        ("type", C.c_int32),
+        ("k", C.c_int32),
+        ("top_word", C.c_void_p),
+        ("top_value", C.c_void_p),
+        ("draws", C.c_int32),
+        ("temperature", C.c_double),
+        ("u", C.c_void_p),
+        ("seed", C.c_uint64),
+        ("step", C.c_uint32),
+        ("draw_word", C.c_void_p),
+        ("draw_logp", C.c_void_p),
     ]
 
 
@@ -133,6 +177,23 @@ def load_library() -> C.CDLL:
     L.spdp_debug_poke.restype = cint
     L.spdp_debug_weight_rows.argtypes = [vp, i64, i64, vp, vp]
     L.spdp_debug_weight_rows.restype = cint
+    L.spdp_pack8.argtypes = [vp, vp, i32, i64, vp]
+    L.spdp_pack8.restype = cint
+    L.spdp_product8.argtypes = [vp, vp, vp, i32, vp, i32, i64]
+    L.spdp_product8.restype = cint
+    L.spdp_adjust.argtypes = [vp, vp, i64, vp, i64, i32, vp]
+    L.spdp_adjust.restype = cint
+    L.spdp_words_work.argtypes = [i64, i32, i32, C.POINTER(i64)]
+    L.spdp_words_work.restype = cint
+    L.spdp_top.argtypes = [vp, vp, i64, i32, i64, i32, vp, i32, vp, vp, vp, i64]
+    L.spdp_top.restype = cint
+    L.spdp_draw.argtypes = [vp, vp, i64, i32, i64, i32, vp, dbl, i32, vp, u64, u32, vp, vp, vp,
+                            i64]
+    L.spdp_draw.restype = cint
+    L.spdp_predict_work.argtypes = [i64, i32, i32, i32, C.POINTER(i64)]
+    L.spdp_predict_work.restype = cint
+    L.spdp_predict.argtypes = [vp, vp, vp, vp, vp, vp, i64]
+    L.spdp_predict.restype = cint
     return L
 
 
@@ -400,6 +461,204 @@ def spdp_align_topics(dist):
 
 
 # ---------------------------------------------------------------------------
+# Words of documents (device tensors; the calls only enqueue on the state's
+# stream, so tensors have to be made and freed in that stream's order)
+# ---------------------------------------------------------------------------
+_TYPE_OF = {"torch.float64": SPDP_F64, "torch.float32": SPDP_F32, "torch.float16": SPDP_F16,
+            "torch.bfloat16": SPDP_BF16}
+_TYPES = {}  # torch dtype -> SPDP_F64 ...
+
+
+def _type(x):
+    t = _TYPES.get(x.dtype)
+    if t is None:
+        t = _TYPE_OF.get(str(x.dtype))
+        if t is None:
+            raise ValueError(f"no such type here: {x.dtype}")
+        _TYPES[x.dtype] = t
+    return t
+
+
+def _matrix(x, what):
+    """(pointer, rows, columns, elements from one row to the next) of a device matrix whose
+    rows are contiguous."""
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError(f"{what}: a device matrix")
+    rows, cols = x.shape
+    ld, step = x.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: elements of a row must be contiguous")
+    if rows <= 1 and ld < cols:
+        ld = cols  # (a single row's stride says nothing)
+    return x.data_ptr(), rows, cols, ld
+
+
+def _vector(x, shape, dtype, what):
+    """Pointer of a contiguous device tensor of this shape and type (None: null)."""
+    if x is None:
+        return None
+    if tuple(x.shape) != shape or str(x.dtype) != dtype or not x.is_cuda or \
+            not x.is_contiguous():
+        raise ValueError(f"{what}: a contiguous device tensor {shape} of {dtype}")
+    return x.data_ptr()
+
+
+class Rows8:
+    """Rows in 8 bits: q [rows, blocks * 128] (torch.float8_e4m3fn) and e [rows, blocks]
+    (uint8, exponent + 127 of each block's scale); see include/spdp.h."""
+
+    def __init__(self, q, e, cols):
+        nb = -(-cols // SPDP_BLOCK8)
+        rows = q.shape[0]
+        self.q, self.e, self.rows, self.cols = q, e, rows, cols
+        self.c = _Rows8(rows, cols,
+                        _vector(q, (rows, nb * SPDP_BLOCK8), "torch.float8_e4m3fn", "q"),
+                        _vector(e, (rows, nb), "torch.uint8", "e"))
+        self.ref = C.addressof(self.c)
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda"):
+        import torch
+
+        nb = -(-cols // SPDP_BLOCK8)
+        return cls(torch.empty((rows, nb * SPDP_BLOCK8), dtype=torch.float8_e4m3fn,
+                               device=device),
+                   torch.empty((rows, nb), dtype=torch.uint8, device=device), cols)
+
+
+class Rules:
+    """Rules on the scores of `rows` documents over n_words words (device tensors, all of
+    them optional; kept by the object):
+
+    doc_off [rows + 1] int64, words [n] int32, penalties [rows, 3] float32 (repeat, presence,
+    frequency); bias [tables, n_words] float32, bias_of [rows] int32; mask [tables,
+    ceil(n_words / 32)] int32 bits, mask_of [rows] int32.  See include/spdp.h."""
+
+    def __init__(self, rows, n_words, doc_off=None, words=None, penalties=None, bias=None,
+                 bias_of=None, mask=None, mask_of=None):
+        i32, f32 = "torch.int32", "torch.float32"
+        tables = [0 if t is None else t.shape[0] for t in (bias, mask)]
+        listed = 0 if words is None else words.shape[0]
+        self.kept = (doc_off, words, penalties, bias, bias_of, mask, mask_of)
+        self.rows, self.n_words = rows, n_words
+        self.c = _Rules(
+            rows, n_words, tables[0], tables[1], listed,
+            _vector(doc_off, (rows + 1,), "torch.int64", "doc_off"),
+            _vector(words, (listed,), i32, "words"),
+            _vector(penalties, (rows, 3), f32, "penalties"),
+            _vector(bias, (tables[0], n_words), f32, "bias"),
+            _vector(bias_of, (rows,), i32, "bias_of"),
+            _vector(mask, (tables[1], -(-n_words // 32)), i32, "mask"),
+            _vector(mask_of, (rows,), i32, "mask_of"))
+        self.ref = C.addressof(self.c)
+
+
+def spdp_pack8(h, x, out: Rows8):
+    """Round rows x [rows, cols] (float64 or float32) to out; returns out."""
+    p, rows, cols, ld = _matrix(x, "x")
+    if (rows, cols) != (out.rows, out.cols):
+        raise ValueError(f"x {rows} x {cols}, out {out.rows} x {out.cols}")
+    _check(lib().spdp_pack8(h, p, _type(x), ld, out.ref))
+    return out
+
+
+def spdp_product8(h, a: Rows8, b: Rows8, out, log: bool = False):
+    """out [a.rows, b.rows] = a b^T, or its logarithm; returns out."""
+    p, rows, cols, ld = _matrix(out, "out")
+    if (rows, cols) != (a.rows, b.rows):
+        raise ValueError(f"out {rows} x {cols} for {a.rows} x {b.rows} products")
+    _check(lib().spdp_product8(h, a.ref, b.ref, 1 if log else 0, p, _type(out), ld))
+    return out
+
+
+def spdp_adjust(h, x, rules: Rules, out):
+    """Scores x under the rules into out (x itself, or another matrix); returns out."""
+    p, rows, cols, ld = _matrix(x, "x")
+    po, rows_o, cols_o, ldo = _matrix(out, "out")
+    if x.dtype != out.dtype or (rows, cols) != (rows_o, cols_o) or \
+            (rows, cols) != (rules.rows, rules.n_words):
+        raise ValueError("x, out and the rules do not agree")
+    _check(lib().spdp_adjust(h, p, ld, po, ldo, _type(x), rules.ref))
+    return out
+
+
+def spdp_words_work(rows: int, n_words: int, take: int = 0) -> int:
+    """Bytes of workspace of spdp_top (take = k) and spdp_draw."""
+    n = C.c_int64()
+    _check(lib().spdp_words_work(int(rows), int(n_words), int(take), C.byref(n)))
+    return n.value
+
+
+def _work(work):
+    if work is None:
+        return None, 0
+    if not work.is_cuda or not work.is_contiguous():
+        raise ValueError("work: a contiguous device tensor")
+    return work.data_ptr(), work.numel() * work.element_size()
+
+
+def spdp_top(h, x, word, value, work, rules: Rules = None):
+    """The best words of every row of x: word [rows, k] int32, value [rows, k] float32;
+    returns both."""
+    p, rows, cols, ld = _matrix(x, "x")
+    k = word.shape[1]
+    _check(lib().spdp_top(h, p, ld, _type(x), rows, cols, rules and rules.ref, k,
+                          _vector(word, (rows, k), "torch.int32", "word"),
+                          _vector(value, (rows, k), "torch.float32", "value"), *_work(work)))
+    return word, value
+
+
+def spdp_draw(h, x, word, logp, work, u=None, rules: Rules = None, temperature: float = 1.0,
+              seed: int = 0, step: int = 0):
+    """Words drawn from every row of x: word [rows, draws] int32, logp [rows, draws] float32,
+    by the uniforms u [rows, draws] float64 or the seed's; returns both."""
+    p, rows, cols, ld = _matrix(x, "x")
+    n = word.shape[1]
+    _check(lib().spdp_draw(h, p, ld, _type(x), rows, cols, rules and rules.ref,
+                           temperature, n, _vector(u, (rows, n), "torch.float64", "u"),
+                           int(seed) & (2**64 - 1), int(step) & 0xFFFFFFFF,
+                           _vector(word, (rows, n), "torch.int32", "word"),
+                           _vector(logp, (rows, n), "torch.float32", "logp"), *_work(work)))
+    return word, logp
+
+
+def spdp_predict_work(docs: int, n_words: int, dtype, k: int = 0) -> int:
+    """Bytes of workspace for a good number of documents at a time."""
+    n = C.c_int64()
+    _check(lib().spdp_predict_work(int(docs), int(n_words), _TYPE_OF[str(dtype)], int(k),
+                                   C.byref(n)))
+    return n.value
+
+
+def spdp_predict(h, docs: Rows8, words: Rows8, work, rules: Rules = None, scores=None,
+                 dtype=None, top=None, drawn=None, temperature: float = 1.0, u=None,
+                 seed: int = 0, step: int = 0):
+    """Words for documents: any of scores [docs, words] (else they are held in `dtype` in the
+    workspace), top = (word, value) [docs, k] and drawn = (word, logp) [docs, draws]."""
+    D, V = docs.rows, words.rows
+    a = _Answer(type=SPDP_F32, temperature=temperature, seed=int(seed) & (2**64 - 1),
+                step=int(step) & 0xFFFFFFFF)
+    if scores is not None:
+        a.scores, rows, cols, a.ld = _matrix(scores, "scores")
+        a.type = _type(scores)
+        if (rows, cols) != (D, V):
+            raise ValueError(f"scores {rows} x {cols} for {D} documents, {V} words")
+    elif dtype is not None:
+        a.type = _TYPE_OF[str(dtype)]
+    if top is not None:
+        a.k = top[0].shape[1]
+        a.top_word = _vector(top[0], (D, a.k), "torch.int32", "word")
+        a.top_value = _vector(top[1], (D, a.k), "torch.float32", "value")
+    if drawn is not None:
+        a.draws = drawn[0].shape[1]
+        a.draw_word = _vector(drawn[0], (D, a.draws), "torch.int32", "word")
+        a.draw_logp = _vector(drawn[1], (D, a.draws), "torch.float32", "logp")
+        a.u = _vector(u, (D, a.draws), "torch.float64", "u")
+    _check(lib().spdp_predict(h, docs.ref, words.ref, rules and rules.ref, C.byref(a),
+                              *_work(work)))
+
+
+# ---------------------------------------------------------------------------
 # Convenience wrapper (host numpy in and out)
 # ---------------------------------------------------------------------------
 class Sampler:
@@ -532,3 +791,50 @@ class Sampler:
         ppl, ll = spdp_heldout(self.h, words, doc_offsets, doc_group, self.G, self.V, n_sweeps,
                                seed, z)
         return ppl, ll, z
+
+    def predict(self, theta, phi, top=0, draws=0, seed=0, step=0, temperature=1.0,
+                doc_words=None, penalties=(1.0, 0.0, 0.0), bias=None, allowed=None):
+        """Words for documents from host estimates theta [D, K] and phi [V, K] (a group's, or
+        phi0): (top words [D, top], their scores, drawn words [D, draws], their log
+        probabilities).  doc_words: a list of word ids for every document, which `penalties`
+        = (repeat, presence, frequency) make less likely; bias [V]: added to the scores;
+        allowed [V]: truth values, the words to choose from."""
+        import torch
+
+        dev = torch.device("cuda", torch.cuda.current_device())
+        put = lambda x, t: torch.as_tensor(np.ascontiguousarray(x, t)).to(dev)  # noqa: E731
+        D, V = len(theta), len(phi)
+        rules = None
+        if doc_words is not None or bias is not None or allowed is not None:
+            r = {}
+            if doc_words is not None:
+                if len(doc_words) != D:
+                    raise ValueError("doc_words: one list per document")
+                r["doc_off"] = put(np.cumsum([0] + [len(w) for w in doc_words]), np.int64)
+                r["words"] = put(np.concatenate([np.asarray(w, np.int32) for w in doc_words] +
+                                                [np.empty(0, np.int32)]), np.int32)
+                r["penalties"] = put(np.broadcast_to(np.asarray(penalties, np.float32), (D, 3)),
+                                     np.float32)
+            if bias is not None:
+                r["bias"] = put(np.reshape(bias, (1, V)), np.float32)
+            if allowed is not None:
+                bits = np.zeros(-(-V // 32) * 32, np.uint8)
+                bits[:V] = np.asarray(allowed, bool)
+                r["mask"] = put(np.packbits(bits, bitorder="little").view("<i4")[None], np.int32)
+            rules = Rules(D, V, **r)
+        packed = []
+        for x in (theta, phi):
+            x = put(x, np.float64)
+            packed.append((x, Rows8.empty(*x.shape, device=dev)))
+        outs = [tuple(torch.empty((D, n), dtype=t, device=dev)
+                      for t in (torch.int32, torch.float32)) for n in (top, draws)]
+        work = torch.empty(spdp_predict_work(D, V, torch.float32, top), dtype=torch.uint8,
+                           device=dev)
+        torch.cuda.synchronize(dev)  # (the state's stream may be another than torch's)
+        for x, to in packed:
+            spdp_pack8(self.h, x, to)
+        spdp_predict(self.h, packed[0][1], packed[1][1], work, rules=rules,
+                     top=outs[0] if top else None, drawn=outs[1] if draws else None,
+                     temperature=temperature, seed=seed, step=step)
+        torch.cuda.synchronize(dev)
+        return tuple(x.cpu().numpy() for pair in outs for x in pair)

@@ -1,0 +1,701 @@
+"""Words of documents on the GPU against the fp64 oracle (oracle/words.py): 8-bit rows and
+their products, rules on scores, best words, draws, and all of them in one call.
+
+Tolerances.  Packed rows, adjusted scores, best words and drawn words are equal to the
+oracle's: a packed value and a rule's step are one rounding each of exact inputs, and a draw
+is compared unless its uniform lies within 1e-11 of a border between two words (the borders
+are sums of up to 10^5 fp64 weights, each off by a few 2^-53 of the total at most).  A
+product's sum of P padded columns takes at most P roundings of 2^-23 of the sum of
+magnitudes (2^-24, or a cut of the last place); its logarithm adds 2^-22 of itself (the
+hardware's base-2 logarithm, its scaling and their roundings); then half a step of the
+output's type.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import synth
+from oracle import words as ow
+from paper_1510_06549_amd import spdp as sp
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f64": torch.float64, "f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def _state(stream=None):
+    return sp.Sampler(np.array([0, 1], np.int32), np.array([0, 2], np.int64),
+                      np.array([0], np.int32), 1, 2, 1, 0.1, 0.5, 1.0, 0.1,
+                      hip_stream=None if stream is None else stream.cuda_stream)
+
+
+@pytest.fixture(scope="module")
+def state():
+    s = _state()
+    yield s
+    s.close()
+
+
+def dev(x, dtype=None):
+    return torch.as_tensor(np.ascontiguousarray(x)).to("cuda", dtype)
+
+
+def framed(rows, cols, dtype, ld=None, at=0, fill=7.0):
+    """(a [rows, cols] view at element `at` of a buffer with rows `ld` apart, the buffer)."""
+    ld = cols if ld is None else ld
+    buf = torch.full((at + rows * ld + 64,), fill, dtype=dtype, device="cuda")
+    return buf[at:at + rows * ld].view(rows, ld)[:, :cols], buf
+
+
+def frame_kept(buf, view, fill=7.0):
+    """Whether everything of the buffer outside the view is as it was."""
+    other = buf.clone()
+    torch.as_strided(other, view.shape, view.stride(), view.storage_offset()).fill_(fill)
+    return bool((other.float() == fill).all())
+
+
+def work_for(rows, n, take=0):
+    return torch.empty(max(16, sp.spdp_words_work(rows, n, take)), dtype=torch.uint8,
+                       device="cuda")
+
+
+# ---------------------------------------------------------------------------
+# rows in 8 bits
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("type", ["f64", "f32"])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (3, 50, 0), (2, 128, 1), (5, 129, 0),
+                                           (9, 500, 3), (2, 1000, 0), (70, 257, 0)])
+def test_pack(state, rows, cols, pad, type):
+    say(f"pack {rows} x {cols} + {pad} {type}")
+    rng = np.random.default_rng(rows * 1000 + cols)
+    x = rng.normal(size=(rows, cols)) * np.exp(rng.normal(size=(rows, cols)) * 6)
+    x[rng.random(x.shape) < 0.1] = 0
+    x[:, 0] = 448.0 if rows > 2 else 3.0
+    if rows >= 3:
+        # ties between neighbouring codes, values of every kind that has no number
+        mid = (ow.VALUES8[:-1] + ow.VALUES8[1:]) / 2
+        n = min(cols - 1, 126)
+        x[1, 1:1 + n] = mid[-n:] if cols < 60 else mid[:n]
+        x[2, :cols // 2] = [np.nan, np.inf, -np.inf, 1e-30, -2.0][:cols // 2] + \
+            [0.5] * max(0, cols // 2 - 5)
+    if rows >= 5:
+        x[3] = 0.0
+        x[4] *= 1e-35
+    x = dev(x, TYPES[type])
+    src, _ = framed(rows, cols, TYPES[type], ld=cols + pad, at=pad)
+    src.copy_(x)
+    nb = -(-cols // 128)
+    qbuf = torch.full((rows * nb * 128 + 256,), 0x55, dtype=torch.uint8, device="cuda")
+    ebuf = torch.full((rows * nb + 64,), 0x55, dtype=torch.uint8, device="cuda")
+    out = sp.Rows8(qbuf[:rows * nb * 128].view(rows, -1).view(torch.float8_e4m3fn),
+                   ebuf[:rows * nb].view(rows, nb), cols)
+    sp.spdp_pack8(state.h, src, out)
+    q, e = ow.pack8(src.double().cpu().numpy())
+    np.testing.assert_array_equal(out.e.cpu().numpy(), e)
+    got = out.q.view(torch.uint8).cpu().numpy()
+    nan = (q & 127) == 127
+    np.testing.assert_array_equal((got & 127) == 127, nan)
+    # (a zero's sign is the value's, or +)
+    np.testing.assert_array_equal(ow.value8(got)[~nan], ow.value8(q)[~nan])
+    assert (qbuf[rows * nb * 128:] == 0x55).all() and (ebuf[rows * nb:] == 0x55).all()
+
+
+def test_pack_rounds_once(state):
+    """Values a hair above and below the middle of two codes: a rounding to fp32 first
+    would make them ties."""
+    say("pack, double rounding")
+    mid = (ow.VALUES8[:-1] + ow.VALUES8[1:]) / 2
+    x = np.concatenate([[448.0], mid[:126], [0.0], [448.0], mid[:126] * (1 + 2.0 ** -40), [0.0],
+                        [448.0], mid[:126] * (1 - 2.0 ** -40)])[None]
+    out = sp.Rows8.empty(1, x.shape[1])
+    sp.spdp_pack8(state.h, dev(x), out)
+    q, e = ow.pack8(x)
+    np.testing.assert_array_equal(out.q.view(torch.uint8).cpu().numpy(), q)
+
+
+def test_pack_empty_and_extremes(state):
+    say("pack, no rows; scales at both ends")
+    sp.spdp_pack8(state.h, torch.empty((0, 9), dtype=torch.float64, device="cuda"),
+                  sp.Rows8.empty(0, 9))
+    x = np.array([[1e300, 1.0], [1e-300, 1e-310], [448 * 2.0 ** 127, -1.0], [2.0 ** -127, 0.0],
+                  [-0.0, 5e-324]])
+    out = sp.Rows8.empty(5, 2)
+    sp.spdp_pack8(state.h, dev(x), out)
+    q, e = ow.pack8(x)
+    np.testing.assert_array_equal(out.e.cpu().numpy(), e)
+    got = ow.value8(out.q.view(torch.uint8).cpu().numpy())
+    np.testing.assert_array_equal(got, ow.value8(q))
+
+
+# ---------------------------------------------------------------------------
+# products
+# ---------------------------------------------------------------------------
+def _packed(rng, rows, cols, spread, sign=False):
+    x = np.exp(rng.normal(size=(rows, cols)) * spread)
+    if sign:
+        x *= rng.choice([-1.0, 1.0], size=x.shape)
+    x[rng.random(x.shape) < 0.05] = 0
+    x *= np.exp(rng.normal(size=(rows, 1)) * 3)
+    q, e = ow.pack8(x)
+    return sp.Rows8(dev(q).view(torch.float8_e4m3fn), dev(e), cols), ow.unpack8(q, e)
+
+
+def _check_product(got, a, b, log, dtype):
+    P = a.shape[1]
+    ref, mag = a @ b.T, np.abs(a) @ np.abs(b).T
+    err = P * 2.0 ** -23 * mag
+    half = torch.finfo(dtype).eps / 2
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps  # last place of zero
+    with np.errstate(all="ignore"):
+        if log:
+            rel = err / ref
+            assert rel[ref > 0].max(initial=0) < 0.01
+            want = np.log(ref)
+            tol = 1.01 * rel + 2.0 ** -22 * (np.abs(want) + 1)
+        else:
+            want, tol = ref, err
+        tol = tol + half * np.abs(want) + tiny
+        most = torch.finfo(dtype).max
+        inner = np.isfinite(want) & (np.abs(want) < most * (1 - half))
+        assert np.all(np.abs(got - want)[inner] <= (tol * (1 + half))[inner]), \
+            (np.abs(got - want) / tol)[inner].max()
+    assert np.array_equal(np.isneginf(got), np.isneginf(want) | (want <= -most * (1 + half)))
+
+
+@pytest.mark.parametrize("m,n,cols", [(1, 1, 1), (1, 17, 50), (16, 16, 128), (17, 33, 129),
+                                      (3, 1000, 500), (130, 257, 300), (65, 129, 1000),
+                                      (300, 700, 513), (2, 5000, 64), (33, 4097, 100),
+                                      (200, 40, 1024), (1000, 3, 20)])
+@pytest.mark.parametrize("type,log", [("f32", True), ("f32", False), ("f16", True),
+                                      ("bf16", False)])
+def test_product(state, m, n, cols, type, log):
+    say(f"product {m} x {n} x {cols} {type} log={log}")
+    rng = np.random.default_rng(m + 10 * n + 100 * cols)
+    a8, a = _packed(rng, m, cols, 2.0)
+    b8, b = _packed(rng, n, cols, 3.0)
+    if type in ("f16",) and not log:
+        pytest.skip("range")
+    for pad, at in ((0, 0), (5, 3)):
+        out, buf = framed(m, n, TYPES[type], ld=n + pad, at=at)
+        sp.spdp_product8(state.h, a8, b8, out, log=log)
+        _check_product(out.double().cpu().numpy(), a, b, log, TYPES[type])
+        assert frame_kept(buf, out)
+
+
+@pytest.mark.parametrize("m,n", [(5, 300), (150, 300)])
+def test_product_signs_zero_rows_and_nan(state, m, n):
+    say(f"product of mixed signs {m} x {n}")
+    rng = np.random.default_rng(3)
+    a8, a = _packed(rng, m, 200, 1.0, sign=True)
+    b8, b = _packed(rng, n, 200, 1.0, sign=True)
+    a8.q[1].zero_()
+    a[1] = 0
+    out = torch.empty((m, n), device="cuda")
+    sp.spdp_product8(state.h, a8, b8, out)
+    _check_product(out.double().cpu().numpy(), a, b, False, torch.float32)
+    assert (out[1] == 0).all()
+    sp.spdp_product8(state.h, a8, b8, out, log=True)
+    got = out.cpu().numpy()
+    assert np.isneginf(got[1]).all()
+    ref = a @ b.T
+    sure = np.abs(ref) > 256 * 2.0 ** -23 * (np.abs(a) @ np.abs(b).T)
+    assert np.array_equal(np.isnan(got)[sure], (ref < 0)[sure])
+    b8.q.view(torch.uint8)[2, 7] = 127  # NaN
+    sp.spdp_product8(state.h, a8, b8, out)
+    got = out.cpu().numpy()
+    assert np.isnan(got[:, 2]).all() and np.isfinite(np.delete(got, 2, 1)).all()
+
+
+def test_product_range_of_scales(state):
+    """Scales from end to end of what fp32 sums hold; probabilities near 1 and far below."""
+    say("product, far scales")
+    rng = np.random.default_rng(4)
+    a = np.abs(rng.normal(size=(20, 300))) + 0.1
+    b = np.abs(rng.normal(size=(40, 300))) + 0.1
+    a[0] *= 1e30
+    a[1, :128] *= 1e-30
+    a[2] *= 1e-30
+    b[3] *= 1e-8
+    b[4, 128:] *= 1e-30
+    a[5], b[5] = 0, 0
+    a[5, 0] = b[5, 0] = 1.0
+    (qa, ea), (qb, eb) = ow.pack8(a), ow.pack8(b)
+    a8 = sp.Rows8(dev(qa).view(torch.float8_e4m3fn), dev(ea), 300)
+    b8 = sp.Rows8(dev(qb).view(torch.float8_e4m3fn), dev(eb), 300)
+    out = torch.empty((20, 40), device="cuda")
+    for log in (False, True):
+        sp.spdp_product8(state.h, a8, b8, out, log=log)
+        _check_product(out.double().cpu().numpy(), ow.unpack8(qa, ea), ow.unpack8(qb, eb), log,
+                       torch.float32)
+
+
+def test_product_empty(state):
+    say("product without rows")
+    a, b = sp.Rows8.empty(0, 5), sp.Rows8.empty(3, 5)
+    sp.spdp_product8(state.h, a, b, torch.empty((0, 3), device="cuda"))
+    sp.spdp_product8(state.h, b, a, torch.empty((3, 0), device="cuda"))
+
+
+# ---------------------------------------------------------------------------
+# rules
+# ---------------------------------------------------------------------------
+def _scores(rng, rows, V, dtype, coarse=False):
+    x = rng.normal(size=(rows, V)) * 3 - 4
+    if coarse:
+        x = np.round(x)
+    return dev(x, dtype)
+
+
+class RuleSet:
+    """Rules for the library and the same for the oracle."""
+
+    def __init__(self, rng, rows, V, listed=True, bias=True, mask=True, shared=False):
+        kw, self.o = {}, {}
+        if listed:
+            docs = [rng.integers(-3, V + 3, size=[0, 1, 30, 200][i % 4]) for i in range(rows)]
+            for i, d in enumerate(docs):
+                if len(d) > 4:
+                    d[:4] = i % V  # a word several times
+            pen = np.stack([1 + rng.random(rows), rng.random(rows), rng.random(rows)], 1)
+            kw.update(doc_off=dev(np.cumsum([0] + [len(d) for d in docs])),
+                      words=dev(np.concatenate(docs).astype(np.int32)),
+                      penalties=dev(pen, torch.float32))
+            self.o.update(listed=docs, penalties=pen.astype(np.float32))
+        if bias:
+            t = rng.normal(size=(3, V)).astype(np.float32)
+            of = np.zeros(rows, int) if shared else rng.integers(-1, 3, size=rows)
+            kw.update(bias=dev(t), bias_of=None if shared else dev(of, torch.int32))
+            self.o["bias"] = np.where(of[:, None] >= 0, t[np.maximum(of, 0)], 0)
+            # (adding 0 changes nothing but a -0)
+        if mask:
+            t = rng.random((4, V)) < 0.6
+            t[2] = False
+            of = np.zeros(rows, int) if shared else rng.integers(-1, 4, size=rows)
+            bits = np.zeros((4, -(-V // 32) * 32), np.uint8)
+            bits[:, :V] = t
+            bits[:, V:] = 1  # bits behind the last word mean nothing
+            kw.update(mask=dev(np.packbits(bits, axis=1, bitorder="little").view("<i4").copy()),
+                      mask_of=None if shared else dev(of, torch.int32))
+            self.o["allowed"] = np.where(of[:, None] >= 0, t[np.maximum(of, 0)], True)
+        self.c = sp.Rules(rows, V, **kw)
+
+    def oracle(self, x):
+        return ow.adjusted(x.float().cpu().numpy(), **self.o)
+
+
+SIZES = [(1, 1), (2, 5), (1, 33), (7, 1000), (3, 4095), (2, 4097), (9, 10007), (130, 70)]
+
+
+@pytest.mark.parametrize("rows,V", SIZES)
+@pytest.mark.parametrize("type", ["f32", "f16", "bf16"])
+def test_adjust(state, rows, V, type):
+    say(f"adjust {rows} x {V} {type}")
+    rng = np.random.default_rng(rows + V)
+    for parts in ((1, 1, 1, 0), (1, 0, 0, 0), (0, 1, 0, 1), (0, 0, 1, 1), (0, 0, 1, 0),
+                  (0, 0, 0, 0)):
+        r = RuleSet(rng, rows, V, *(bool(p) for p in parts))
+        for pad, at in ((0, 0), (3, 1)):
+            x, xbuf = framed(rows, V, TYPES[type], ld=V + pad, at=at)
+            x.copy_(_scores(rng, rows, V, TYPES[type]))
+            want = torch.from_numpy(r.oracle(x)).to(TYPES[type])
+            y, ybuf = framed(rows, V, TYPES[type], ld=V + 2 * pad, at=2 * at)
+            before = xbuf.clone()
+            sp.spdp_adjust(state.h, x, r.c, y)
+            torch.testing.assert_close(y.cpu(), want, rtol=0, atol=0)
+            assert frame_kept(ybuf, y) and torch.equal(before, xbuf)
+            sp.spdp_adjust(state.h, x, r.c, x)  # in place
+            torch.testing.assert_close(x.cpu(), want, rtol=0, atol=0)
+            assert frame_kept(xbuf, x)
+
+
+def test_adjust_scores_without_a_number(state):
+    say("adjust: infinities, NaN, lowest values, masked and not")
+    for type in ("f32", "f16", "bf16"):
+        big = torch.finfo(TYPES[type]).max
+        row = [np.nan, np.inf, -np.inf, -big, big, 0.0, -0.0, 1.0]
+        x = dev(np.array([row, row, row]), TYPES[type])
+        rng = np.random.default_rng(0)
+        r = RuleSet(rng, 3, 8, listed=False, bias=False, mask=False)
+        mask = dev(np.array([[0], [0xFF], [0b10101010]], np.int32))
+        pen = dev(np.array([[2.0, 1.0, 0.5]] * 3, np.float32))
+        r = sp.Rules(3, 8, mask=mask, mask_of=dev(np.arange(3, dtype=np.int32)), penalties=pen,
+                     doc_off=dev(np.array([0, 8, 16, 24])),
+                     words=dev(np.tile(np.arange(8), 3).astype(np.int32)))
+        got = sp.spdp_adjust(state.h, x, r, torch.empty_like(x)).cpu()
+        allowed = np.array([[0] * 8, [1] * 8, [0, 1] * 4], bool)
+        want = torch.from_numpy(ow.adjusted(x.float().cpu().numpy(), [range(8)] * 3,
+                                            [[2.0, 1.0, 0.5]] * 3, None, allowed)).to(TYPES[type])
+        torch.testing.assert_close(got, want, rtol=0, atol=0, equal_nan=True)
+        assert torch.isneginf(got[0]).all()
+
+
+def test_rules_out_of_range(state):
+    """Indices past their tables make the row NaN; offsets are clamped; nothing out of the
+    arrays is read."""
+    say("rules out of range")
+    V = 50
+    x = torch.zeros((6, V), device="cuda")
+    bias = torch.ones((2, V), device="cuda")
+    mask = dev(np.full((2, 2), -1, np.int32))
+    of = dev(np.array([0, 1, 2, -1, -5, 2 ** 31 - 1], np.int32))
+    for kw in (dict(bias=bias, bias_of=of), dict(mask=mask, mask_of=of)):
+        y = sp.spdp_adjust(state.h, x, sp.Rules(6, V, **kw), torch.empty_like(x))
+        assert torch.isnan(y).all(1).tolist() == [False, False, True, False, False, True]
+        word, value = torch.empty((6, 2), dtype=torch.int32, device="cuda"), \
+            torch.empty((6, 2), device="cuda")
+        sp.spdp_top(state.h, x, word, value, work_for(6, V, 2), rules=sp.Rules(6, V, **kw))
+        assert word[2].tolist() == [-1, -1] and word[0].tolist() == [0, 1]
+        sp.spdp_draw(state.h, x, word, value, work_for(6, V), rules=sp.Rules(6, V, **kw))
+        assert (word[5] == -1).all() and torch.isnan(value[5]).all() and (word[0] >= 0).all()
+    off = dev(np.array([-7, 2, 1, 3, 99, 2 ** 40, 4]))
+    words = dev(np.array([0, 1, 2, 3], np.int32))
+    pen = dev(np.tile(np.array([1.0, 1.0, 0.0], np.float32), (6, 1)))
+    r = sp.Rules(6, V, doc_off=off, words=words, penalties=pen)
+    y = sp.spdp_adjust(state.h, x, r, torch.empty_like(x)).cpu().numpy()
+    lists = [[0, 1], [], [1, 2], [3], [], []]
+    want = np.zeros((6, V))
+    for i, w in enumerate(lists):
+        want[i, w] = -1
+    np.testing.assert_array_equal(y, want)
+
+
+def test_long_lists(state):
+    """A document longer than its vocabulary, and counts beyond 16 bits."""
+    say("adjust with 200 000 listed words")
+    rng = np.random.default_rng(5)
+    V = 5000
+    docs = [np.full(150000, 4097), rng.integers(0, V, 50000)]
+    pen = np.array([[1.5, 0.25, 2.0 ** -10]] * 2, np.float32)
+    x = _scores(rng, 2, V, torch.float32)
+    r = sp.Rules(2, V, doc_off=dev(np.array([0, 150000, 200000])),
+                 words=dev(np.concatenate(docs).astype(np.int32)), penalties=dev(pen))
+    y = sp.spdp_adjust(state.h, x, r, torch.empty_like(x)).cpu().numpy()
+    np.testing.assert_array_equal(y, ow.adjusted(x.cpu().numpy(), docs, pen))
+
+
+# ---------------------------------------------------------------------------
+# best words
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,V", SIZES + [(40, 20000)])
+@pytest.mark.parametrize("k", [1, 7, 64, 256])
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+def test_top(state, rows, V, k, type):
+    say(f"top {k} of {rows} x {V} {type}")
+    rng = np.random.default_rng(rows + V + k)
+    for coarse in (False, True):  # many ties
+        x, _ = framed(rows, V, TYPES[type], ld=V + 3, at=1)
+        x.copy_(_scores(rng, rows, V, TYPES[type], coarse))
+        for r in (None, RuleSet(rng, rows, V, bias=not coarse)):
+            want = ow.top(x.float().cpu().numpy() if r is None else r.oracle(x), k)
+            word, wbuf = framed(rows, k, torch.int32, fill=9)
+            value, vbuf = framed(rows, k, torch.float32)
+            sp.spdp_top(state.h, x, word, value, work_for(rows, V, k), rules=r and r.c)
+            np.testing.assert_array_equal(word.cpu().numpy(), want[0])
+            np.testing.assert_array_equal(value.cpu().numpy(), want[1])
+            assert frame_kept(wbuf, word, 9) and frame_kept(vbuf, value)
+
+
+@pytest.mark.parametrize("V", [9, 300, 9000])
+def test_top_special_rows(state, V):
+    say(f"top: rows of one value, sorted rows, infinities, {V} words")
+    x = np.zeros((9, V), np.float32)
+    x[1] = np.arange(V)
+    x[2] = -np.arange(V)
+    x[3] = -np.inf
+    x[4] = np.nan
+    x[5, ::2] = -0.0  # ties with 0
+    x[6, V // 2:] = np.inf
+    x[7] = -np.inf
+    x[7, V - 1] = -3.0e38
+    x[8] = np.nan
+    x[8, V // 2] = -np.inf
+    x[8, V - 2] = -1
+    for k in (1, 5, 256):
+        want = ow.top(x, k)
+        word = torch.empty((9, k), dtype=torch.int32, device="cuda")
+        value = torch.empty((9, k), device="cuda")
+        sp.spdp_top(state.h, dev(x), word, value, work_for(9, V, k))
+        np.testing.assert_array_equal(word.cpu().numpy(), want[0])
+        np.testing.assert_array_equal(value.cpu().numpy(), want[1])
+
+
+# ---------------------------------------------------------------------------
+# draws
+# ---------------------------------------------------------------------------
+def _check_draws(word, logp, x, u, temperature, most_skipped=0.01):
+    ww, wl, gap = ow.drawn(x, u, temperature)
+    sure = ~(gap <= 1e-11)
+    assert (~sure).mean() <= most_skipped, (~sure).sum()
+    np.testing.assert_array_equal(word[sure], ww[sure])
+    law = ww >= 0
+    assert np.array_equal(np.isnan(logp), ~law)
+    # one rounding to fp32 of a logarithm whose fp64 error is far below it
+    ok = sure & law
+    assert np.all(np.abs(logp - wl)[ok] <= 2.0 ** -24 * 1.001 * np.abs(wl)[ok] + 1e-12)
+
+
+@pytest.mark.parametrize("rows,V", SIZES + [(3, 100000)])
+@pytest.mark.parametrize("n", [1, 5, 300])
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+def test_draw(state, rows, V, n, type):
+    say(f"draw {n} of {rows} x {V} {type}")
+    rng = np.random.default_rng(rows + V + n)
+    for r, temperature in ((None, 1.0), (True, 1.0), (None, 0.25), (True, 3.0)):
+        x, _ = framed(rows, V, TYPES[type], ld=V + 3, at=1)
+        x.copy_(_scores(rng, rows, V, TYPES[type]))
+        r = r and RuleSet(rng, rows, V)
+        u = rng.random((rows, n))
+        u[0, 0] = 0.0
+        word, wbuf = framed(rows, n, torch.int32, fill=9)
+        logp, lbuf = framed(rows, n, torch.float32)
+        sp.spdp_draw(state.h, x, word, logp, work_for(rows, V), u=dev(u), rules=r and r.c,
+                     temperature=temperature)
+        xo = x.float().cpu().numpy() if r is None else r.oracle(x)
+        _check_draws(word.cpu().numpy(), logp.cpu().numpy(), xo, u, temperature)
+        assert frame_kept(wbuf, word, 9) and frame_kept(lbuf, logp)
+
+
+@pytest.mark.parametrize("V", [6, 5000, 9000])
+def test_draw_special_rows(state, V):
+    """Rows without a law, a single allowed word, weights that vanish in most places, and
+    uniforms at and outside the ends."""
+    say(f"draw: special rows, {V} words")
+    x = np.zeros((9, V), np.float32)
+    x[0] = -np.inf
+    x[1, 3] = np.nan
+    x[2, V - 1] = np.inf
+    x[3] = -np.inf
+    x[3, V - 2] = -1e30                 # the only word
+    x[4] = -800.0 * np.arange(V)        # all weight on word 0
+    x[5] = -800.0 * np.arange(V)[::-1]  # all weight on the last word
+    x[6, V // 2:] = -740.0              # weights near the smallest fp64
+    x[7] = -3.0e38
+    x[8, ::2] = -np.inf
+    u = np.tile(np.array([0.0, 0.3, 1 - 2.0 ** -53, 1.0, 2.0, -1.0, np.nan, np.inf]), (9, 1))
+    word = torch.empty((9, 8), dtype=torch.int32, device="cuda")
+    logp = torch.empty((9, 8), device="cuda")
+    sp.spdp_draw(state.h, dev(x), word, logp, work_for(9, V), u=dev(u))
+    got = word.cpu().numpy()
+    ww, wl, _ = ow.drawn(x, u)
+    # the last word with weight is where 1 - 2^-53 may fall too, or the one before a border
+    np.testing.assert_array_equal(np.delete(got, 2, 1), np.delete(ww, 2, 1))
+    assert np.all((got[:, 2] >= 0) == (ww[:, 2] >= 0)) and np.all(got[3] == V - 2)
+    assert np.array_equal(np.isnan(logp.cpu().numpy()), ww < 0)
+    assert (got[:3] == -1).all() and (got[4] == 0).all() and (got[5] == V - 1).all()
+    assert (got[8] % 2 == 1).all()
+
+
+def test_draw_by_seed(state):
+    say("draw by seed")
+    rng = np.random.default_rng(8)
+    rows, V, n, seed, step = 5, 3000, 40, 0x123456789ABCDEF, 7
+    x = _scores(rng, rows, V, torch.float32)
+    word = torch.empty((rows, n), dtype=torch.int32, device="cuda")
+    logp = torch.empty((rows, n), device="cuda")
+    sp.spdp_draw(state.h, x, word, logp, work_for(rows, V), seed=seed, step=step)
+    u = np.array([oracle.philox_word0(seed, i, step, 4) for i in range(rows * n)])
+    _check_draws(word.cpu().numpy(), logp.cpu().numpy(), x.cpu().numpy(),
+                 u.reshape(rows, n) * 2.0 ** -32, 1.0)
+
+
+def test_no_rows_and_no_draws(state):
+    say("top and draw of nothing")
+    x = torch.empty((0, 50), device="cuda")
+    e = lambda *s, dtype: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+    w = work_for(0, 50, 3)
+    sp.spdp_top(state.h, x, e(0, 3, dtype=torch.int32), e(0, 3, dtype=torch.float32), w)
+    sp.spdp_draw(state.h, x, e(0, 3, dtype=torch.int32), e(0, 3, dtype=torch.float32), w)
+    x = torch.zeros((2, 50), device="cuda")
+    sp.spdp_draw(state.h, x, e(2, 0, dtype=torch.int32), e(2, 0, dtype=torch.float32),
+                 work_for(2, 50))
+    sp.spdp_adjust(state.h, e(0, 50, dtype=torch.float32), sp.Rules(0, 50),
+                   e(0, 50, dtype=torch.float32))
+
+
+# ---------------------------------------------------------------------------
+# refusals that need a device
+# ---------------------------------------------------------------------------
+def test_refusals_on_device(state):
+    say("refusals on the device")
+    x = torch.zeros((4, 100), device="cuda")
+    word = torch.empty((4, 3), dtype=torch.int32, device="cuda")
+    value = torch.empty((4, 3), device="cuda")
+
+    def refused(text, call, *a, **kw):
+        with pytest.raises(sp.SpdpError) as e:
+            call(*a, **kw)
+        assert e.value.code == sp.SPDP_E_ARG and text in str(e.value), str(e.value)
+
+    r = sp.Rules(4, 100)
+    both = torch.zeros(1000, device="cuda")
+    refused("overlap", sp.spdp_adjust, state.h, both[:400].view(4, 100), r,
+            both[100:500].view(4, 100))
+    refused("a workspace of", sp.spdp_top, state.h, x, word, value,
+            torch.empty(16, dtype=torch.uint8, device="cuda"))
+    refused("a workspace of", sp.spdp_draw, state.h, x, word, value, None)
+    refused("aligned", sp.spdp_draw, state.h, x, word, value,
+            torch.empty(1 << 16, dtype=torch.uint8, device="cuda")[8:])
+    refused("rules for 3 x 100", sp.spdp_top, state.h, x, word, value, work_for(4, 100, 3),
+            rules=sp.Rules(3, 100))
+    refused("need doc_off", sp.spdp_adjust, state.h, x,
+            sp.Rules(4, 100, penalties=torch.ones((4, 3), device="cuda")), x)
+    refused("without penalties", sp.spdp_adjust, state.h, x, sp.Rules(
+        4, 100, doc_off=torch.zeros(5, dtype=torch.int64, device="cuda"),
+        words=torch.zeros(1, dtype=torch.int32, device="cuda")), x)
+    refused("without its table", sp.spdp_adjust, state.h, x, sp.Rules(
+        4, 100, mask_of=torch.zeros(4, dtype=torch.int32, device="cuda")), x)
+    L = sp.lib()
+    host = np.zeros((4, 100), np.float32)
+    assert L.spdp_adjust(state.h, host.ctypes.data, 100, x.data_ptr(), 100, sp.SPDP_F32,
+                         r.ref) == sp.SPDP_E_ARG and "x is not device" in sp.spdp_last_error()
+    # rows far past the allocation
+    big = sp._Rules(rows=1 << 30, n_words=100)
+    import ctypes
+    assert L.spdp_adjust(state.h, x.data_ptr(), 100, x.data_ptr(), 100, sp.SPDP_F32,
+                         ctypes.addressof(big)) == sp.SPDP_E_ARG
+    assert "run past its allocation" in sp.spdp_last_error()
+
+
+# ---------------------------------------------------------------------------
+# all of them
+# ---------------------------------------------------------------------------
+def _model(rng, D, V, K):
+    theta = rng.dirichlet(np.full(K, 0.1), size=D)
+    phi = rng.dirichlet(np.full(V, 0.05), size=K).T + 1e-9
+    out = []
+    for x in (theta, phi):
+        q, e = ow.pack8(x)
+        out.append(sp.Rows8(dev(q).view(torch.float8_e4m3fn), dev(e), K))
+    return out
+
+
+def _outs(D, n):
+    return (torch.full((D, n), -7, dtype=torch.int32, device="cuda"),
+            torch.full((D, n), 7.0, device="cuda"))
+
+
+@pytest.mark.parametrize("D,V,K", [(1, 500, 10), (37, 5001, 50), (130, 9000, 200)])
+def test_predict_is_its_steps(state, D, V, K):
+    say(f"predict {D} x {V} x {K}")
+    rng = np.random.default_rng(D + V)
+    docs, words = _model(rng, D, V, K)
+    r = RuleSet(rng, D, V)
+    u = dev(rng.random((D, 9)))
+    for type in ("f32", "bf16"):
+        t = TYPES[type]
+        scores = torch.empty((D, V), dtype=t, device="cuda")
+        sp.spdp_product8(state.h, docs, words, scores, log=True)
+        want_top, want_drawn = _outs(D, 20), _outs(D, 9)
+        sp.spdp_top(state.h, scores, *want_top, work_for(D, V, 20), rules=r.c)
+        sp.spdp_draw(state.h, scores, *want_drawn, work_for(D, V), u=u, rules=r.c)
+        # with room for all documents, for one, and for some
+        full = sp.spdp_predict_work(D, V, t, 20)
+        one = -(-V * scores.element_size() // 256) * 256 + sp.spdp_words_work(1, V, 20)
+        for room in {full, one, min(full, 5 * one + 100)}:
+            top, drawn = _outs(D, 20), _outs(D, 9)
+            work = torch.empty(room, dtype=torch.uint8, device="cuda")
+            sp.spdp_predict(state.h, docs, words, work, rules=r.c, dtype=t, top=top, drawn=drawn,
+                            u=u)
+            for a, b in zip(top + drawn, want_top + want_drawn):
+                assert torch.equal(a.nan_to_num(5.0), b.nan_to_num(5.0))
+        with pytest.raises(sp.SpdpError):
+            sp.spdp_predict(state.h, docs, words, work[:one - 256], rules=r.c, dtype=t, top=top)
+        # the scores are kept: adjusted, and the words come from them
+        sp.spdp_adjust(state.h, scores, r.c, scores)
+        kept, buf = framed(D, V, t, ld=V + 5, at=3)
+        top = _outs(D, 20)
+        sp.spdp_predict(state.h, docs, words, work_for(D, V, 20), rules=r.c, scores=kept, top=top)
+        assert torch.equal(kept, scores) and frame_kept(buf, kept)
+        want = _outs(D, 20)
+        sp.spdp_top(state.h, scores, *want, work_for(D, V, 20))
+        for a, b in zip(top, want):
+            assert torch.equal(a, b)
+        if type == "f32":
+            for a, b in zip(top, want_top):
+                assert torch.equal(a, b)
+    # seeded draws do not depend on how many documents are held at a time
+    drawn = [_outs(D, 3) for _ in range(2)]
+    for d, room in zip(drawn, (sp.spdp_predict_work(D, V, t), one)):
+        sp.spdp_predict(state.h, docs, words, torch.empty(room, dtype=torch.uint8, device="cuda"),
+                        dtype=t, drawn=d, seed=5, step=1)
+    assert all(torch.equal(a, b) for a, b in zip(*drawn))
+
+
+def test_predict_of_a_trained_state():
+    """From counts to words: estimates, 8-bit rows, scores, rules, words, against the
+    oracle on the estimates themselves."""
+    say("words of a trained state")
+    wl = synth.workload(0)
+    cp = synth.generate(wl, 0)
+    s = sp.Sampler(cp.words, cp.doc_off, cp.doc_group, cp.n_groups, cp.vocab, wl.K, wl.alpha,
+                   wl.a, wl.b, wl.gamma)
+    for sweep in range(20):
+        s.sweep(sweep, 3)
+    theta, _, phi = s.estimates(0, 1)
+    docs = [d for d in range(len(cp.doc_group)) if cp.doc_group[d] == 0][:40]
+    lists = [cp.words[cp.doc_off[d]:cp.doc_off[d + 1]] for d in docs]
+    allowed = np.ones(cp.vocab, bool)
+    allowed[::7] = False
+    word, value, dw, dl = s.predict(theta[docs], phi[0], top=10, draws=200, seed=11,
+                                    doc_words=lists, penalties=(1.0, 50.0, 0.0), allowed=allowed)
+    exact = np.log(theta[docs] @ phi[0].T)
+    # a value in 8 bits is off by 2^-4 at most (or 2^-10 of its block's scale, far below
+    # the sums here), a product of two by (1 + 2^-4)^2, its logarithm by 0.13
+    for i, w in enumerate(lists):
+        seen = np.isin(np.arange(cp.vocab), w)
+        want = np.where(allowed, exact[i] - 50.0 * seen, -np.inf)
+        assert np.all(np.abs(value[i] - want[word[i]]) <= 0.13)
+        assert not np.isin(word[i], w).any() and allowed[word[i]].all()
+        best = np.sort(want)[::-1][:10]
+        assert np.all(np.abs(value[i] - best) <= 0.13)
+        assert allowed[dw[i]].all() and not np.isin(dw[i], w).any()
+    again = s.predict(theta[docs], phi[0], draws=200, seed=11, doc_words=lists,
+                      penalties=(1.0, 50.0, 0.0), allowed=allowed)
+    assert np.array_equal(again[2], dw) and again[0].shape == (40, 0)
+    assert s.check() == 0
+    s.close()
+
+
+def test_captured_and_on_streams():
+    """A captured chain, replayed between eager calls with other inputs, and two states on
+    streams of their own with workspaces of their own."""
+    say("captured words")
+    rng = np.random.default_rng(12)
+    D, V, K = 20, 5000, 60
+    stream = torch.cuda.Stream()
+    s, e = _state(stream), _state()
+    theta = [dev(rng.dirichlet(np.full(K, 0.2), size=D)) for _ in range(3)]
+    _, words = _model(rng, 1, V, K)
+    r = RuleSet(rng, D, V)
+    u = dev(rng.random((D, 9)))
+
+    def chain(h, x, packed, work, outs):
+        sp.spdp_pack8(h, x, packed)
+        sp.spdp_predict(h, packed, words, work, rules=r.c, top=outs[0], drawn=outs[1], u=u)
+
+    def room():
+        return (sp.Rows8.empty(D, K), torch.empty(sp.spdp_predict_work(D, V, torch.float32, 20),
+                                                  dtype=torch.uint8, device="cuda"),
+                (_outs(D, 20), _outs(D, 9)))
+
+    x = theta[0].clone()
+    mine, other = room(), room()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        chain(s.h, x, *mine)
+    for t in theta + theta[:1]:
+        with torch.cuda.stream(stream):
+            x.copy_(t)
+            graph.replay()
+        chain(e.h, t, *other)  # at the same time, on the null stream
+        torch.cuda.synchronize()
+        for a, b in zip(mine[2][0] + mine[2][1], other[2][0] + other[2][1]):
+            assert torch.equal(a.nan_to_num(5.0), b.nan_to_num(5.0))
+    s.close()
+    e.close()
