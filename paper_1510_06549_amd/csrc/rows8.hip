@@ -71,6 +71,7 @@ __global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, int64_t 
 typedef __bf16 b2v __attribute__((ext_vector_type(2)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
 typedef float f4v __attribute__((ext_vector_type(4)));
+typedef int i4v __attribute__((ext_vector_type(4)));
 
 // 8 packed values times their block's scale as bf16.  This rounds nothing for scales of
 // 2^-124 to 2^119: a value has 4 significant bits, and bf16 has the exponents of fp32.
@@ -98,42 +99,391 @@ __device__ __forceinline__ _Float16 out_as<_Float16>(float v) { return (_Float16
 template <>
 __device__ __forceinline__ __bf16 out_as<__bf16>(float v) { return (__bf16)v; }
 
-// c[i][j] = sum_k a[i][k] b[j][k], or its logarithm: one wavefront per 16 x 16
-// outputs.  A lane gives 8 columns of row (lane & 15) of either operand to an
-// instruction; which columns does not matter to the sum as long as both operands
-// agree.
-template <typename T, bool LOG>
-__global__ void __launch_bounds__(256) k_product8(const uint8_t *__restrict__ aq,
-                                                  const uint8_t *__restrict__ ae, int64_t m,
-                                                  const uint8_t *__restrict__ bq,
-                                                  const uint8_t *__restrict__ be, int64_t n,
-                                                  int32_t nb, T *__restrict__ c, int64_t ld,
-                                                  int64_t tiles_j, int64_t tiles)
+// Natural logarithms of N sums: the hardware's base-2 logarithm (1 ulp, normal
+// arguments only) times log 2.  Sums below the normal range, zeros and negative ones
+// among them, are rare enough to be looked for in all of a wavefront's sums at once.
+template <int N>
+__device__ __forceinline__ void log_of(float (&v)[N])
 {
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (tile >= tiles) return;
-    const int lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4;
-    const int64_t i0 = tile / tiles_j * 16, j0 = tile % tiles_j * 16;
-    // rows past the end repeat the last one; their outputs are not stored
-    const int64_t ia = i0 + r < m ? i0 + r : m - 1, jb = j0 + r < n ? j0 + r : n - 1;
-    const uint8_t *pa = aq + ia * nb * kBlock + part * 32, *pb = bq + jb * nb * kBlock + part * 32;
+    constexpr float kLog2 = 0.693147180559945f;
+    float least = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) least = fminf(least, v[i]);
+    if (__any(least < 0x1p-126f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool tiny = v[i] < 0x1p-126f;
+            const float l = __builtin_amdgcn_logf(tiny ? v[i] * 0x1p+32f : v[i]);
+            v[i] = (tiny ? l - 32.f : l) * kLog2;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_logf(v[i]) * kLog2;
+    }
+}
+
+// N values at c, whose address is aligned to one value.
+template <typename T, int N>
+__device__ __forceinline__ void store_n(T *c, const T (&v)[N])
+{
+    __builtin_memcpy(c, v, sizeof v);
+}
+
+// 16 bytes at p, whose address is aligned to 2; STREAM: past the caches' usual order.
+template <bool STREAM, typename T>
+__device__ __forceinline__ void store_unit(T *p, i4v v)
+{
+    typedef int unit __attribute__((ext_vector_type(4), aligned(2)));
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<unit *>(p));
+    else *reinterpret_cast<unit *>(p) = v;
+}
+
+// c[i][j] = sum_k a[i][k] b[j][k], or its logarithm, for documents a and words b.
+//
+// A workgroup keeps 16 FD documents in LDS, converted to bf16 once and laid out as
+// the matrix instructions read them (every read is 64 lanes x 16 bytes in a row).
+// Its eight wavefronts then go over the words on their own, without a barrier, 64
+// words at a time: words come from memory in 8 bits straight into the registers of
+// the one wavefront that uses them, a block of 128 columns ahead of the products,
+// and are converted there.  So one wavefront's stores and logarithms run under
+// another's products, LDS is read once per FW products, and a word is converted once
+// per 16 FD documents.
+//
+// Instruction j (of 4) of a block sums the columns 32 p + 8 j .. + 7, p = 0 .. 3
+// (p = lane / 16): a lane's 32 bytes of a row lie together.  The order of a sum does not
+// depend on FW and FD, nor an output on how many rows are multiplied at a time.
+//
+// Words are the matrix instruction's rows, so that a lane ends with words that lie
+// next to each other in c; the words of a wavefront are dealt to its fragments so that
+// they make stores of kPer values, 16 bytes where FW allows.
+//
+// Columns past kLdsBlocks / FD blocks do not fit the LDS at once: then documents are
+// staged again, part by part, for every round of words.
+constexpr int kWordFragments = 4;
+constexpr int kLdsBlocks = 32;  // (blocks of columns) x (document fragments) in 128 KB
+
+template <typename T, bool LOG, int FD, bool STREAM>
+__global__ void __launch_bounds__(512, 2) k_product8(
+    const uint8_t *__restrict__ aq, const uint8_t *__restrict__ ae, int32_t m,
+    const uint8_t *__restrict__ bq, const uint8_t *__restrict__ be, int32_t n, int32_t nb,
+    T *__restrict__ c, int64_t ld, int32_t tiles_d, int32_t ranges, int32_t rounds)
+{
+    constexpr int FW = kWordFragments;
+    constexpr int kPer = 16 / sizeof(T);      // values of a store
+    constexpr int kJoin = kPer / 4;           // fragments of a store
+    constexpr int kMost = kLdsBlocks / FD;    // blocks in LDS at a time
+    extern __shared__ uint4 docs[];           // [block][j][document fragment][lane]
+    // Workgroups go to the 8 XCDs in turn; each XCD takes consecutive ones of the order
+    // (range, documents), so that its workgroups read the same words at a time.
+    const int32_t total = tiles_d * ranges, per = (total + 7) / 8;
+    const int32_t order = (int32_t)(blockIdx.x & 7) * per + (int32_t)(blockIdx.x >> 3);
+    if ((int32_t)(blockIdx.x >> 3) >= per || order >= total) return;
+    const int32_t d0 = order % tiles_d * (16 * FD), range = order / tiles_d;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, part = lane >> 4;
+    const int64_t pitch = (int64_t)nb * kBlock;
+
+    auto stage = [&](int32_t b0, int32_t blocks) {
+        for (int u = wave; u < blocks * FD; u += 8) {
+            const int b = u / FD, y = u % FD;
+            // (documents past the end repeat the last one; nothing of them is stored)
+            const int32_t d = d0 + y * 16 + r < m ? d0 + y * 16 + r : m - 1;
+            const uint4 *q = reinterpret_cast<const uint4 *>(aq + d * pitch +
+                                                             (int64_t)(b0 + b) * kBlock + part * 32);
+            const uint4 lo = q[0], hi = q[1];
+            const float f = scale_of(ae[(int64_t)d * nb + b0 + b]);
+            b8v *to = reinterpret_cast<b8v *>(docs) + (b * 4 * FD + y) * 64 + lane;
+            to[0] = unpack8(lo.x, lo.y, f);
+            to[FD * 64] = unpack8(lo.z, lo.w, f);
+            to[2 * FD * 64] = unpack8(hi.x, hi.y, f);
+            to[3 * FD * 64] = unpack8(hi.z, hi.w, f);
+        }
+    };
+    const bool fits = nb <= kMost;
+
+    // This wavefront's words of a round: fragment x, row r.  The last tile is moved back
+    // to be a whole one (its first words are then made twice, the same).
+    uint32_t off[FW], eoff[FW];
+#pragma unroll
+    for (int x = 0; x < FW; ++x) {
+        const uint32_t row = x / kJoin * (16 * kJoin) + (r >> 2) * kPer + x % kJoin * 4 + (r & 3);
+        off[x] = row * (uint32_t)pitch + part * 32;
+        eoff[x] = row * (uint32_t)nb;
+    }
+    auto first_word = [&](int32_t tile) {
+        const int32_t w0 = tile * (16 * FW);
+        return w0 > n - 16 * FW ? n - 16 * FW : w0;
+    };
+    uint4 q[FW][2];
+    uint32_t scale[FW];
+    // (half a block of the next block's columns is requested as soon as the present
+    // block's half is converted)
+    auto request = [&](int32_t w0, int32_t b, int half) {
+        const uint8_t *wq = bq + w0 * pitch + (int64_t)b * kBlock + 16 * half;
+        const uint8_t *we = be + w0 * (int64_t)nb + b;
+#pragma unroll
+        for (int x = 0; x < FW; ++x) {
+            q[x][half] = *reinterpret_cast<const uint4 *>(wq + off[x]);
+            if (half) scale[x] = we[eoff[x]];
+        }
+    };
+    b8v fw[FW], fd[2];
+    float f[FW];
+    auto convert = [&](int j) {
+#pragma unroll
+        for (int x = 0; x < FW; ++x) {
+            const uint4 v = q[x][j >> 1];
+            fw[x] = j & 1 ? unpack8(v.z, v.w, f[x]) : unpack8(v.x, v.y, f[x]);
+        }
+    };
+    const b8v *held = reinterpret_cast<const b8v *>(docs) + lane;
+    const int32_t tiles_w = (n + 16 * FW - 1) / (16 * FW), stride = ranges * 8;
+    int32_t tile = range * 8 + wave;
+    int32_t w0 = first_word(tile < tiles_w ? tile : 0);
+    if (fits) {
+        stage(0, nb);
+        __syncthreads();
+    }
+    request(w0, 0, 0);
+    request(w0, 0, 1);
+    fd[0] = held[0];
+    fd[1] = held[64];
+    for (int32_t round = 0; round < rounds; ++round, tile += stride) {
+        if (fits && tile >= tiles_w) return;
+        const bool here = tile < tiles_w;
+        // (past the last tile, the present one is requested again)
+        const int32_t then_w0 = first_word(tile + stride < tiles_w ? tile + stride : here ? tile : 0);
+        f4v acc[FW][FD];
+#pragma unroll
+        for (int x = 0; x < FW; ++x)
+#pragma unroll
+            for (int y = 0; y < FD; ++y) acc[x][y] = f4v{0.f, 0.f, 0.f, 0.f};
+        for (int32_t b0 = 0; b0 < nb; b0 += kMost) {
+            const int32_t b1 = b0 + kMost < nb ? b0 + kMost : nb;
+            if (!fits) {
+                __syncthreads();
+                stage(b0, b1 - b0);
+                __syncthreads();
+                if (!here) continue;
+                fd[0] = held[0];
+                fd[1] = held[64];
+            }
+            for (int32_t b = b0; b < b1; ++b) {
+                const b8v *now = held + (b - b0) * 4 * FD * 64;
+                const b8v *then = b + 1 < b1 ? now + 4 * FD * 64 : held;
+                const int32_t next_b = b + 1 < nb ? b + 1 : 0, next_w0 = b + 1 < nb ? w0 : then_w0;
+#pragma unroll
+                for (int x = 0; x < FW; ++x) f[x] = scale_of(scale[x]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    convert(j);
+                    if (j & 1) request(next_w0, next_b, j >> 1);
+#pragma unroll
+                    for (int y = 0; y < FD; ++y) {
+                        const int i = j * FD + y;
+                        const b8v d = fd[i & 1];
+                        fd[i & 1] = i + 2 < 4 * FD ? now[(i + 2) * 64] : then[(i + 2 - 4 * FD) * 64];
+#pragma unroll
+                        for (int x = 0; x < FW; ++x)
+                            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[x], d, acc[x][y],
+                                                                                0, 0, 0);
+                        if constexpr (FD >= 4) {  // one LDS read ahead of every FW products
+                            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x008, FW, 0);
+                        }
+                    }
+                }
+            }
+        }
+        if (!here) continue;
+        // Value v of a lane: word row 4 part + v of the fragment, document column r.  A unit
+        // of kPer words of a document is a 16-byte store; four lanes have a document's
+        // unit u side by side.  Lanes r and r ^ 8 trade units u and u + 1, so that a store
+        // instruction writes 128 bytes of 8 documents and not 64 of 16.
+#pragma unroll
+        for (int y = 0; y < FD; ++y) {
+            float v[4 * FW];
+#pragma unroll
+            for (int i = 0; i < 4 * FW; ++i) v[i] = acc[i / 4][y][i % 4];
+            if constexpr (LOG) log_of(v);
+            const bool hi = r & 8;
+            const int32_t d = d0 + y * 16 + (r & 7);
+            T *to = c + d * ld + w0 + (hi ? 16 * kJoin : 0) + part * kPer;
+#pragma unroll
+            for (int u = 0; u < FW / kJoin; u += 2) {
+                i4v one[2];  // units u and u + 1 of document r
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    T out[kPer];
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) out[i] = out_as<T>(v[(u + e) * kPer + i]);
+                    __builtin_memcpy(&one[e], out, sizeof out);
+                }
+                i4v low, high;  // unit u (hi: u + 1) of documents r & 7 and (r & 7) + 8
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int got = __builtin_amdgcn_mov_dpp(hi ? one[0][i] : one[1][i],
+                                                             0x128, 0xF, 0xF, true);  // ror 8
+                    low[i] = hi ? got : one[0][i];
+                    high[i] = hi ? one[1][i] : got;
+                }
+                if (d < m) store_unit<STREAM>(to + u * 16 * kJoin, low);
+                if (d + 8 < m) store_unit<STREAM>(to + 8 * ld + u * 16 * kJoin, high);
+            }
+        }
+        w0 = then_w0;
+    }
+}
+
+// The same for few documents, or few words: a wavefront makes 16 x 16 outputs.  Here the
+// words' bytes are all there is to wait for, so four blocks of them are requested at
+// once, by as many wavefronts as the chip holds, before the documents' blocks are
+// converted into LDS for the workgroup's four wavefronts.  (Documents read from the
+// caches by every wavefront instead: 17.3 us for 16 x 100 000 x 500, 12.4 so.)
+template <typename T, bool LOG>
+__global__ void __launch_bounds__(256) k_product8_few(
+    const uint8_t *__restrict__ aq, const uint8_t *__restrict__ ae, int32_t m,
+    const uint8_t *__restrict__ bq, const uint8_t *__restrict__ be, int32_t n, int32_t nb,
+    T *__restrict__ c, int64_t ld, int32_t tiles_d)
+{
+    constexpr int kAhead = 4;
+    __shared__ b8v docs[kAhead][4][64];  // [block][j][lane]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, part = lane >> 4;
+    const int64_t d0 = (int64_t)(blockIdx.x % tiles_d) * 16;
+    const int64_t w0 = ((int64_t)(blockIdx.x / tiles_d) * 4 + wave) * 16;
+    const int64_t pitch = (int64_t)nb * kBlock;
+    // (rows past the end repeat the last one; nothing of them is stored)
+    const int64_t d = d0 + r < m ? d0 + r : m - 1, w = w0 + r < n ? w0 + r : n - 1;
+    const uint4 *qd = reinterpret_cast<const uint4 *>(aq + d * pitch + part * 32);
+    const uint4 *qw = reinterpret_cast<const uint4 *>(bq + w * pitch + part * 32);
+    const uint8_t *ed = ae + d * nb, *ew = be + w * nb;
     f4v acc = {0.f, 0.f, 0.f, 0.f};
-    for (int32_t b = 0; b < nb; ++b) {
-        const float sa = scale_of(ae[ia * nb + b]), sb = scale_of(be[jb * nb + b]);
-        for (int h = 0; h < 2; ++h) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(pa + b * kBlock + 16 * h);
-            const uint4 y = *reinterpret_cast<const uint4 *>(pb + b * kBlock + 16 * h);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack8(x.x, x.y, sa),
-                                                          unpack8(y.x, y.y, sb), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack8(x.z, x.w, sa),
-                                                          unpack8(y.z, y.w, sb), acc, 0, 0, 0);
+    for (int32_t b = 0; b < nb; b += kAhead) {
+        uint4 x[kAhead][2];
+        uint32_t scale[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int32_t at = b + i < nb ? b + i : nb - 1;
+            x[i][0] = qw[at * 8];
+            x[i][1] = qw[at * 8 + 1];
+            scale[i] = ew[at];
+        }
+        if (b) __syncthreads();
+        if (b + wave < nb) {
+            const uint4 lo = qd[(b + wave) * 8], hi = qd[(b + wave) * 8 + 1];
+            const float f = scale_of(ed[b + wave]);
+            docs[wave][0][lane] = unpack8(lo.x, lo.y, f);
+            docs[wave][1][lane] = unpack8(lo.z, lo.w, f);
+            docs[wave][2][lane] = unpack8(hi.x, hi.y, f);
+            docs[wave][3][lane] = unpack8(hi.z, hi.w, f);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (b + i >= nb) break;
+            const float f = scale_of(scale[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 v = x[i][j >> 1];
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    j & 1 ? unpack8(v.z, v.w, f) : unpack8(v.x, v.y, f), docs[i][j][lane], acc, 0,
+                    0, 0);
+            }
         }
     }
-    // result: value v of a lane is row 4 (lane >> 4) + v, column lane & 15
-    if (j0 + r >= n) return;
-    for (int v = 0; v < 4; ++v) {
-        const int64_t i = i0 + 4 * part + v;
-        if (i < m) c[i * ld + j0 + r] = out_as<T>(LOG ? logf(acc[v]) : acc[v]);
+    float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+    if constexpr (LOG) log_of(v);
+    if (d0 + r >= m || w0 >= n) return;
+    T out[4], *to = c + (d0 + r) * ld + w0 + part * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = out_as<T>(v[i]);
+    if (w0 + 16 <= n) {
+        store_n(to, out);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (w0 + part * 4 + i < n) to[i] = out[i];
+    }
+}
+
+// How a product is shared out: document tiles, workgroups that share a document
+// tile's words, and the rounds of words that each of their wavefronts takes.
+struct Shares {
+    int64_t tiles_d, ranges, rounds;
+};
+
+Shares shares_of(int64_t m, int64_t n, int32_t fd)
+{
+    const int64_t tw = (n + 16 * kWordFragments - 1) / (16 * kWordFragments), most = (tw + 7) / 8;
+    Shares s;
+    s.tiles_d = (m + 16 * fd - 1) / (16 * fd);
+    // a workgroup for each of the 256 compute units; where there are several times as
+    // many tiles of documents, some more, to end together
+    s.ranges = s.tiles_d <= 32 ? 256 / s.tiles_d : (1024 + s.tiles_d - 1) / s.tiles_d;
+    if (s.ranges > most) s.ranges = most;
+    s.rounds = (tw + 8 * s.ranges - 1) / (8 * s.ranges);
+    return s;
+}
+
+// Scores above this many bytes are written past the caches' order.  Below, they stay in
+// the last level cache for whoever reads them next, and take less time too (777 x
+// 14 724 in fp16, 23 MB: 11.2 us, 15.0 streamed); above, they would push out the words,
+// which every tile of documents reads again (2 000 x 100 000 in bf16, 400 MB: 237 us, 192
+// streamed; 1 000 x 100 000 of 64 topics in fp16, 200 MB: 72 and 56 us).
+constexpr int64_t kStreamBytes = 64 << 20;
+
+template <typename T, bool LOG, int FD, bool STREAM>
+hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
+{
+    const int32_t nb = blocks8(a.cols), held = nb < kLdsBlocks / FD ? nb : kLdsBlocks / FD;
+    const Shares s = shares_of(a.rows, b.rows, FD);
+    const int64_t per = (s.tiles_d * s.ranges + 7) / 8;
+    static const hipError_t room = hipFuncSetAttribute(
+        reinterpret_cast<const void *>(&k_product8<T, LOG, FD, STREAM>),
+        hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBlocks * 4096);
+    if (room != hipSuccess) return room;
+    hipLaunchKernelGGL((k_product8<T, LOG, FD, STREAM>), dim3((unsigned)(per * 8)), dim3(512),
+                       held * FD * 4096, st, a.q, a.e, (int32_t)a.rows, b.q, b.e, (int32_t)b.rows,
+                       nb, (T *)c, ld, (int32_t)s.tiles_d, (int32_t)s.ranges, (int32_t)s.rounds);
+    return hipGetLastError();
+}
+
+template <typename T, bool LOG, int FD>
+hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
+{
+    return a.rows * b.rows * (int64_t)sizeof(T) > kStreamBytes
+               ? product<T, LOG, FD, true>(a, b, c, ld, st)
+               : product<T, LOG, FD, false>(a, b, c, ld, st);
+}
+
+// Document fragments of a workgroup: those with which the longest wavefront has the
+// least to do, a round taking as long as its products or 3 more document fragments' (its
+// words' conversion and stores).
+template <typename T, bool LOG>
+hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
+{
+    if (a.rows <= 16 || b.rows < 16 * kWordFragments) {
+        const int64_t td = (a.rows + 15) / 16, blocks = td * ((b.rows + 63) / 64);
+        hipLaunchKernelGGL((k_product8_few<T, LOG>), dim3((unsigned)blocks), dim3(256), 0, st, a.q,
+                           a.e, (int32_t)a.rows, b.q, b.e, (int32_t)b.rows, blocks8(a.cols), (T *)c,
+                           ld, (int32_t)td);
+        return hipGetLastError();
+    }
+    int32_t best = 0;
+    int64_t least = INT64_MAX;
+    for (int32_t fd : {2, 4, 6, 8}) {
+        const Shares s = shares_of(a.rows, b.rows, fd);
+        const int64_t over = (s.tiles_d * s.ranges + 255) / 256;
+        const int64_t cost = s.rounds * over * (fd + 3);
+        if (cost < least) {
+            least = cost;
+            best = fd;
+        }
+    }
+    switch (best) {
+        case 2: return product<T, LOG, 2>(a, b, c, ld, st);
+        case 4: return product<T, LOG, 4>(a, b, c, ld, st);
+        case 6: return product<T, LOG, 6>(a, b, c, ld, st);
+        default: return product<T, LOG, 8>(a, b, c, ld, st);
     }
 }
 
@@ -141,16 +491,7 @@ template <typename T>
 hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, bool log, void *c, int64_t ld,
                    hipStream_t st)
 {
-    const int64_t tj = (b.rows + 15) / 16, tiles = (a.rows + 15) / 16 * tj;
-    const dim3 grid((unsigned)((tiles + 3) / 4));
-    const int32_t nb = blocks8(a.cols);
-    if (log)
-        hipLaunchKernelGGL((k_product8<T, true>), grid, dim3(256), 0, st, a.q, a.e, a.rows, b.q,
-                           b.e, b.rows, nb, (T *)c, ld, tj, tiles);
-    else
-        hipLaunchKernelGGL((k_product8<T, false>), grid, dim3(256), 0, st, a.q, a.e, a.rows, b.q,
-                           b.e, b.rows, nb, (T *)c, ld, tj, tiles);
-    return hipGetLastError();
+    return log ? product<T, true>(a, b, c, ld, st) : product<T, false>(a, b, c, ld, st);
 }
 
 }  // namespace
