@@ -11,33 +11,41 @@
 // The steps are rounded one by one (no fused multiply-add), so that the kernels
 // that store the result and those that choose from it see the same scores.
 //
-// A row is taken in chunks of kChunk words by workgroups of kThreads threads.
-// The counts c of a chunk's words are made in LDS: the workgroup walks the
-// document's words and counts those that fall into the chunk (integer atomics,
-// so the order does not matter).
+// A row is taken in chunks by workgroups, 16 bytes of scores a load.  Few words of a
+// chunk are listed: a bitmap in LDS says which, and only for those is a count kept,
+// cleared and added up (integer atomics, so their order does not matter) by walking
+// the document's words twice.
 #pragma once
 
 #include "spdp_internal.hpp"
 
 namespace spdp {
 
-constexpr int kThreads = 256;
-constexpr int kChunk = 4096;
-
-template <typename T, int N>
-struct alignas(sizeof(T)) Pack {
+// 16 bytes of scores from any element's address (gfx950 reads and writes wide words
+// at addresses that are aligned to their parts only).
+template <typename T>
+struct Vec {
+    static constexpr int N = 16 / sizeof(T);
     T v[N];
 };
 
-// N consecutive values from any element's address (gfx950 reads and writes wide
-// words at addresses that are aligned to their parts only).
-template <typename T, int N>
-__device__ __forceinline__ void load_n(const T *p, float (&out)[N])
+template <typename T>
+__device__ __forceinline__ Vec<T> load_vec(const T *p)
 {
-    Pack<T, N> k;
-    __builtin_memcpy(&k, p, sizeof k);
-#pragma unroll
-    for (int i = 0; i < N; ++i) out[i] = (float)k.v[i];
+    typedef int unit __attribute__((ext_vector_type(4), aligned(2)));
+    const auto u = *reinterpret_cast<const unit *>(p);
+    Vec<T> k;
+    __builtin_memcpy(&k, &u, sizeof k);
+    return k;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(T *p, const Vec<T> &k)
+{
+    typedef int unit __attribute__((ext_vector_type(4), aligned(2)));
+    unit u;
+    __builtin_memcpy(&u, &k, sizeof k);
+    *reinterpret_cast<unit *>(p) = u;
 }
 
 // The rules of one row.
@@ -53,7 +61,7 @@ struct RowRules {
 __device__ __forceinline__ RowRules row_rules(const spdp_rules &r, int64_t row)
 {
     RowRules o;
-    if (r.doc_off && r.penalties) {
+    if (r.doc_off) {
         int64_t a = r.doc_off[row], b = r.doc_off[row + 1];
         a = a < 0 ? 0 : a;
         b = b > r.n_listed ? r.n_listed : b;
@@ -78,33 +86,120 @@ __device__ __forceinline__ RowRules row_rules(const spdp_rules &r, int64_t row)
     return o;
 }
 
-// Counts of the words [w0, w0 + kChunk) among the row's listed words.  All threads
-// of the workgroup call it; the counts can be read when it returns.
-__device__ __forceinline__ void chunk_counts(const RowRules &r, int64_t w0, int32_t *count)
+// Score x of a word that is listed c > 0 times.
+__device__ __forceinline__ float penalised(const RowRules &r, float x, int32_t c)
 {
-    for (int i = threadIdx.x; i < kChunk; i += kThreads) count[i] = 0;
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < r.n_words; i += kThreads) {
-        const int64_t at = (int64_t)r.words[i] - w0;
-        if (at >= 0 && at < kChunk) atomicAdd(&count[at], 1);
-    }
-    __syncthreads();
+#pragma clang fp contract(off)
+    const float y = x > 0.f ? x / r.repeat : x * r.repeat;
+    const float fc = r.frequency * (float)c;
+    const float amount = r.presence + fc;
+    return y - amount;
 }
 
 // Score x of word w with count c under the rules.
 __device__ __forceinline__ float ruled(const RowRules &r, float x, int64_t w, int32_t c)
 {
-#pragma clang fp contract(off)
     if (r.bad) return __builtin_nanf("");
-    if (c > 0) {
-        const float y = x > 0.f ? x / r.repeat : x * r.repeat;
-        const float fc = r.frequency * (float)c;
-        const float amount = r.presence + fc;
-        x = y - amount;
-    }
+    if (c > 0) x = penalised(r, x, c);
     if (r.bias) x = x + r.bias[w];
     if (r.mask && !((r.mask[w >> 5] >> (w & 31)) & 1u)) x = -__builtin_inff();
     return x;
 }
+
+// The chunk of a row that a workgroup of THREADS threads holds, PER scores a thread in
+// vectors of 16 bytes: vector u of a thread is at (u THREADS + thread) N of the chunk.
+template <typename T, int THREADS, int PER>
+struct Chunk {
+    static constexpr int kWords = THREADS * PER, N = Vec<T>::N, U = PER / N;
+    struct Listed {  // LDS
+        uint32_t seen[kWords / 32];
+        int32_t count[kWords];
+    };
+    Vec<T> raw[U];
+
+    static __device__ __forceinline__ int at(int u) { return (u * THREADS + (int)threadIdx.x) * N; }
+
+    // Request the scores of words w0 ..; past the row's end none is read.
+    __device__ __forceinline__ void request(const T *row, int64_t w0, int64_t V)
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t w = w0 + at(u);
+            if (w + N <= V) {
+                raw[u] = load_vec(row + w);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) raw[u].v[i] = w + i < V ? row[w + i] : (T)0;
+            }
+        }
+    }
+
+    // Counts of the chunk's words among the row's listed words.  All threads of the
+    // workgroup call it (with the same row); the counts can be read when it returns, and
+    // a barrier has to come before it is called again.
+    static __device__ __forceinline__ void count(const RowRules &r, int64_t w0, Listed &l)
+    {
+        for (int i = threadIdx.x; i < kWords / 32; i += THREADS) l.seen[i] = 0;
+        for (int64_t i = threadIdx.x; i < r.n_words; i += THREADS) {
+            const int64_t a = (int64_t)r.words[i] - w0;
+            if (a >= 0 && a < kWords) l.count[a] = 0;
+        }
+        __syncthreads();
+        for (int64_t i = threadIdx.x; i < r.n_words; i += THREADS) {
+            const int64_t a = (int64_t)r.words[i] - w0;
+            if (a >= 0 && a < kWords) {
+                atomicAdd(&l.count[a], 1);
+                atomicOr(&l.seen[a >> 5], 1u << (a & 31));
+            }
+        }
+        __syncthreads();
+    }
+
+    // The scores of vector u under the rules; -inf past the row's end.
+    __device__ __forceinline__ void scores(const RowRules &r, int64_t w0, int64_t V,
+                                           const Listed &l, int u, float (&x)[N]) const
+    {
+        const int a = at(u);
+        const int64_t w = w0 + a;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (float)raw[u].v[i];
+        if (w + N > V) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool seen = r.n_words > 0 && (l.seen[a >> 5] >> ((a & 31) + i) & 1u);
+                x[i] = w + i < V ? ruled(r, x[i], w + i, seen ? l.count[a + i] : 0)
+                                 : -__builtin_inff();
+            }
+            return;
+        }
+        if (r.n_words > 0) {
+            const uint32_t seen = l.seen[a >> 5] >> (a & 31);
+            if (seen & ((1u << N) - 1)) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (seen >> i & 1u) x[i] = penalised(r, x[i], l.count[a + i]);
+            }
+        }
+        if (r.bias) {
+            typedef float quad __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                const quad b = *reinterpret_cast<const quad *>(r.bias + w + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[i + k] = x[i + k] + b[k];
+            }
+        }
+        if (r.mask) {
+            // (w is a multiple of N, so its bits lie in one byte)
+            const uint32_t ok = reinterpret_cast<const uint8_t *>(r.mask)[w >> 3] >> (w & 7);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = ok >> i & 1u ? x[i] : -__builtin_inff();
+        }
+        if (r.bad) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = __builtin_nanf("");
+        }
+    }
+};
 
 }  // namespace spdp
