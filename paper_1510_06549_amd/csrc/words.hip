@@ -8,7 +8,7 @@ namespace {
 typedef unsigned long long u64;
 
 // One workgroup per (row, chunk).
-constexpr int kAdjustThreads = 256;
+constexpr int kAdjustThreads = 512;
 
 template <typename T>
 __global__ void __launch_bounds__(kAdjustThreads) k_adjust(const T *x, int64_t ldx, T *y,
@@ -60,30 +60,91 @@ __device__ __forceinline__ u64 key_of(uint32_t order, int64_t w)
     return order ? (u64)order << 32 | (uint32_t)~(uint32_t)w : 0;
 }
 
-// The k best of the keys in buf [0, n), best first, to its front; n <= kKeys.  A bitonic
-// sort of the next power of two of them.  All threads call it, with barriers before
-// (the keys are written) and after (they can be read).
 constexpr int kTopThreads = 256;
-constexpr int kKeys = 2048;
+constexpr int kTopWaves = kTopThreads / 64;
+constexpr int kKeys = 2048;  // kept at a time in LDS
 
-__device__ __forceinline__ void sort_keys(u64 *buf, int n)
+struct Kept {  // LDS
+    u64 key[kKeys];
+    int in_wave[2][kTopWaves];
+    int n;
+};
+
+// Cuts the n keys (k < n <= kKeys) down to the k largest, kept.n of them in any order (less
+// than k where there are not so many but 0), and returns a bound that only they reach:
+// the largest that k keys reach, found bit by bit from the first bit that not all keys have
+// alike until exactly k reach it.  All threads call it, behind a barrier; there is one
+// before it returns.
+__device__ __forceinline__ u64 cut_keys(Kept &kept, int n, int k)
 {
-    int size = 2;
-    while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += kTopThreads) buf[i] = 0;
-    for (int k = 2; k <= size; k *= 2)
-        for (int d = k / 2; d; d /= 2) {
-            __syncthreads();
-            for (int p = threadIdx.x; p < size / 2; p += kTopThreads) {
-                const int i = 2 * p - (p & (d - 1)), j = i + d;  // bit d of i is 0
-                const u64 x = buf[i], y = buf[j];
-                if ((x < y) == ((i & k) == 0)) {
-                    buf[i] = y;
-                    buf[j] = x;
-                }
-            }
+    constexpr int kPer = kKeys / kTopThreads;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 key[kPer];
+    u64 any = 0, all = ~0ull;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int at = threadIdx.x + i * kTopThreads;
+        key[i] = at < n ? kept.key[at] : 0;
+        if (at < n) {
+            any |= key[i];
+            all &= key[i];
         }
+    }
+    for (int d = 32; d; d >>= 1) {
+        any |= __shfl_xor(any, d);
+        all &= __shfl_xor(all, d);
+    }
     __syncthreads();
+    if (lane == 0) {
+        kept.key[2 * wave] = any;
+        kept.key[2 * wave + 1] = all;
+    }
+    __syncthreads();
+    for (int i = 0; i < kTopWaves; ++i) {
+        any |= kept.key[2 * i];
+        all &= kept.key[2 * i + 1];
+    }
+    const u64 differ = any ^ all;
+    u64 bit = differ ? 1ull << (63 - __builtin_clzll(differ)) : 0;
+    u64 bound = differ ? all & ~(2 * bit - 1) : all;
+    for (int turn = 0; bit; bit >>= 1, turn ^= 1) {
+        const u64 t = bound | bit;
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) reach += __builtin_popcountll(__ballot(key[i] >= t));
+        if (lane == 0) kept.in_wave[turn][wave] = reach;
+        __syncthreads();
+        reach = 0;
+        for (int i = 0; i < kTopWaves; ++i) reach += kept.in_wave[turn][i];
+        if (reach >= k) bound = t;
+        if (reach == k) break;
+    }
+    bound = bound ? bound : 1;
+    if (threadIdx.x == 0) kept.n = 0;
+    __syncthreads();
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) mine += key[i] >= bound;
+    if (mine) {
+        int to = atomicAdd(&kept.n, mine);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (key[i] >= bound) kept.key[to++] = key[i];
+    }
+    __syncthreads();
+    return bound;
+}
+
+// Calls put(rank, key) for the k largest of the n keys, n <= kTopThreads: a key's rank is
+// the number of larger ones.
+template <typename F>
+__device__ __forceinline__ void rank_keys(const Kept &kept, int n, int k, F put)
+{
+    if ((int)threadIdx.x >= n) return;
+    const u64 key = kept.key[threadIdx.x];
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += kept.key[i] > key;
+    if (rank < k) put(rank, key);
 }
 
 __device__ __forceinline__ void put_top(u64 key, int32_t *word, float *value)
@@ -94,15 +155,15 @@ __device__ __forceinline__ void put_top(u64 key, int32_t *word, float *value)
                  : -__builtin_inff();
 }
 
-// One workgroup per part of a row: `per` chunks, one after another.  What could be among
-// the k best is collected in LDS: keys at or above a bound that at least k of the scores
-// seen so far reach, namely the least of the largest scores that groups of threads have
+// One workgroup per part of a row: `words` words, a chunk at a time.  What could be among
+// the k best is collected in LDS: scores at or above a bound that at least k of those seen
+// so far reach, namely the least of the largest scores that groups of threads have
 // seen, with at least k groups.  The bound rises as the groups see more, so that after
 // the first chunk few scores pass.  Where the collection would overflow (many ties), it
-// is cut down to its k best, which raise the bound to the last of them.
+// is cut down to its k best, again and again.
 template <typename T>
 __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ x, int64_t ld,
-                                                          int64_t V, int32_t parts, int32_t per,
+                                                          int64_t V, int32_t parts, int64_t words,
                                                           spdp_rules rules, int32_t k,
                                                           u64 *__restrict__ best,
                                                           int32_t *__restrict__ word,
@@ -110,42 +171,48 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
 {
     using C = Chunk<T, kTopThreads, 16>;
     __shared__ typename C::Listed listed;
-    __shared__ u64 buf[kKeys];
-    __shared__ uint32_t wave_least[kTopThreads / 64];
-    __shared__ int kept, passing;
+    __shared__ Kept kept;
+    __shared__ uint32_t wave_least[kTopWaves];
+    __shared__ int passing;
     const int64_t row = blockIdx.x / (uint32_t)parts;
-    const int32_t part = blockIdx.x % (uint32_t)parts;
-    const RowRules r = row_rules(rules, row);
-    const int64_t chunks = (V + C::kWords - 1) / C::kWords, first = (int64_t)part * per;
-    const int64_t last = first + per < chunks ? first + per : chunks;
-    int group = 1;  // threads of a group: the most that leaves k groups
-    while (kTopThreads / (2 * group) >= k) group *= 2;
-    if (threadIdx.x == 0) kept = 0;
-    uint32_t mine = 0;    // largest order that this thread has seen
-    u64 bound = 1;        // keys below are not among the k best (1: every word's key passes)
+    const int64_t first = (int64_t)(blockIdx.x % (uint32_t)parts) * words;
+    const int64_t end = first + words < V ? first + words : V;
+    x += row * ld;
     C c;
-    if (first < last) c.request(x + row * ld, first * C::kWords, V);
-    for (int64_t ch = first; ch < last; ++ch) {
-        const int64_t w0 = ch * C::kWords;
+    c.request(x, first, end);
+    const RowRules r = row_rules(rules, row);
+    // threads that hold words of the first chunk, and the largest groups of which there
+    // are k (no group: fewer than k threads; then every score passes)
+    const int64_t holding = (end - first + C::N - 1) / C::N;
+    const int threads = holding < kTopThreads ? (int)holding : kTopThreads;
+    int group = 1;
+    while (group < kTopThreads && (threads + 2 * group - 1) / (2 * group) >= k) group *= 2;
+    const bool grouped = threads >= k, holds = (int)threadIdx.x < threads;
+    if (threadIdx.x == 0) kept.n = 0;
+    uint32_t mine = 0;   // largest order that this thread has seen
+    u64 bound = 1;       // keys below are not among the k best
+    for (int64_t w0 = first; w0 < end; w0 += C::kWords) {
         if (r.n_words > 0) C::count(r, w0, listed);
-        float v[C::U][C::N];
-#pragma unroll
-        for (int u = 0; u < C::U; ++u) c.scores(r, w0, V, listed, u, v[u]);
-        if (ch + 1 < last) c.request(x + row * ld, w0 + C::kWords, V);
         uint32_t order[C::U][C::N];
 #pragma unroll
-        for (int u = 0; u < C::U; ++u)
+        for (int u = 0; u < C::U; ++u) {
+            float v[C::N];
+            c.scores(r, w0, end, listed, u, v);
 #pragma unroll
             for (int i = 0; i < C::N; ++i) {
-                order[u][i] = order_of(v[u][i]);
+                order[u][i] = order_of(v[i]);
                 mine = order[u][i] > mine ? order[u][i] : mine;
             }
+        }
+        if (w0 + C::kWords < end) c.request(x, w0 + C::kWords, end);
         // least of the groups' largest
-        uint32_t g = mine;
+        uint32_t g = holds ? mine : 0;
         for (int d = 1; d < group && d < 64; d *= 2) {
             const uint32_t o = __shfl_xor(g, d);
             g = o > g ? o : g;
         }
+        // (a group without words does not count)
+        if ((int)(threadIdx.x / group * group) >= threads) g = ~0u;
         for (int d = 1; d < 64; d *= 2) {
             const uint32_t o = __shfl_xor(g, d);
             g = o < g ? o : g;
@@ -153,41 +220,34 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
         if ((threadIdx.x & 63) == 0) wave_least[threadIdx.x >> 6] = g;
         if (threadIdx.x == 0) passing = 0;
         __syncthreads();
-        {
-            uint32_t w[kTopThreads / 64];
-#pragma unroll
-            for (int i = 0; i < kTopThreads / 64; ++i) w[i] = wave_least[i];
-            uint32_t least;
-            if (group <= 64) {
-                least = min(min(w[0], w[1]), min(w[2], w[3]));
-            } else if (group == 128) {
-                least = min(max(w[0], w[1]), max(w[2], w[3]));
-            } else {
-                least = max(max(w[0], w[1]), max(w[2], w[3]));
-            }
+        if (grouped) {
+            const uint32_t *w = wave_least;
+            const uint32_t least = group <= 64    ? min(min(w[0], w[1]), min(w[2], w[3]))
+                                   : group == 128 ? min(max(w[0], w[1]), max(w[2], w[3]))
+                                                  : max(max(w[0], w[1]), max(w[2], w[3]));
             const u64 b = (u64)least << 32;
             bound = b > bound ? b : bound;
         }
-        int n = 0;
+        const uint32_t low = (uint32_t)(bound >> 32) > 1 ? (uint32_t)(bound >> 32) : 1;
+        uint32_t pass = 0;
 #pragma unroll
         for (int u = 0; u < C::U; ++u)
 #pragma unroll
             for (int i = 0; i < C::N; ++i)
-                n += key_of(order[u][i], w0 + C::at(u) + i) >= bound;
-        if (n) atomicAdd(&passing, n);
+                pass |= (uint32_t)(order[u][i] >= low) << (u * C::N + i);
+        if (pass) atomicAdd(&passing, __builtin_popcount(pass));
         __syncthreads();
-        const int have = kept;
-        if (have + passing <= kKeys) {
-            __syncthreads();
-            if (n) {
-                int to = atomicAdd(&kept, n);
+        const int room = kKeys - kept.n - passing;
+        __syncthreads();
+        if (room >= 0) {
+            if (pass) {
+                int to = atomicAdd(&kept.n, __builtin_popcount(pass));
 #pragma unroll
                 for (int u = 0; u < C::U; ++u)
 #pragma unroll
-                    for (int i = 0; i < C::N; ++i) {
-                        const u64 key = key_of(order[u][i], w0 + C::at(u) + i);
-                        if (key >= bound) buf[to++] = key;
-                    }
+                    for (int i = 0; i < C::N; ++i)
+                        if (pass >> (u * C::N + i) & 1u)
+                            kept.key[to++] = key_of(order[u][i], w0 + C::at(u) + i);
             }
             __syncthreads();
             continue;
@@ -197,31 +257,37 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
         for (int u = 0; u < C::U; ++u)
 #pragma unroll
             for (int i = 0; i < C::N; i += 4) {
-                __syncthreads();
-                const int m = kept;
+                const int m = kept.n;
                 __syncthreads();  // (everybody has read it)
                 if (m > kKeys / 2) {
-                    sort_keys(buf, m);
-                    if (m >= k) bound = buf[k - 1] > bound ? buf[k - 1] : bound;
-                    __syncthreads();
-                    if (threadIdx.x == 0) kept = m < k ? m : k;
-                    __syncthreads();
+                    const u64 b = cut_keys(kept, m, k);
+                    bound = b > bound ? b : bound;
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const u64 key = key_of(order[u][i + e], w0 + C::at(u) + i + e);
-                    if (key >= bound) buf[atomicAdd(&kept, 1)] = key;
+                    if (key >= bound) kept.key[atomicAdd(&kept.n, 1)] = key;
                 }
+                __syncthreads();
             }
-        __syncthreads();
     }
     __syncthreads();
-    const int n = kept;
-    sort_keys(buf, n);
-    for (int t = threadIdx.x; t < k; t += kTopThreads) {
-        const u64 key = t < n ? buf[t] : 0;
-        if (parts == 1) put_top(key, word + row * k + t, value + row * k + t);
-        else best[(int64_t)blockIdx.x * k + t] = key;
+    int n = kept.n;
+    __syncthreads();
+    if (n > kTopThreads) {
+        cut_keys(kept, n, k);
+        n = k;
+    }
+    word += row * k;
+    value += row * k;
+    best += (int64_t)blockIdx.x * k;
+    rank_keys(kept, n, k, [&](int rank, u64 key) {
+        if (parts == 1) put_top(key, word + rank, value + rank);
+        else best[rank] = key;
+    });
+    for (int t = n + threadIdx.x; t < k; t += kTopThreads) {
+        if (parts == 1) put_top(0, word + t, value + t);
+        else best[t] = 0;
     }
 }
 
@@ -230,19 +296,33 @@ __global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict_
                                                           int32_t k, int32_t *__restrict__ word,
                                                           float *__restrict__ value)
 {
-    __shared__ u64 buf[kKeys];
+    __shared__ Kept kept;
     const int64_t row = blockIdx.x;
+    best += row * n;
     int have = 0;
     for (int64_t from = 0; from < n;) {
         const int take = (int)(n - from < kKeys - have ? n - from : kKeys - have);
-        for (int i = threadIdx.x; i < take; i += kTopThreads) buf[have + i] = best[row * n + from + i];
+        for (int i = threadIdx.x; i < take; i += kTopThreads) kept.key[have + i] = best[from + i];
         from += take;
+        have += take;
         __syncthreads();
-        sort_keys(buf, have + take);
-        have = have + take < k ? have + take : k;
+        if (have > kTopThreads) {
+            cut_keys(kept, have, k);
+            have = kept.n;
+        }
     }
-    for (int t = threadIdx.x; t < k; t += kTopThreads)
-        put_top(t < have ? buf[t] : 0, word + row * k + t, value + row * k + t);
+    word += row * k;
+    value += row * k;
+    rank_keys(kept, have, k, [&](int rank, u64 key) {
+        // (several places may hold no word: they share the rank behind the last word)
+        if (key) put_top(key, word + rank, value + rank);
+    });
+    __shared__ int found;
+    if (threadIdx.x == 0) found = 0;
+    __syncthreads();
+    if ((int)threadIdx.x < have && kept.key[threadIdx.x]) atomicAdd(&found, 1);
+    __syncthreads();
+    for (int t = found + threadIdx.x; t < k; t += kTopThreads) put_top(0, word + t, value + t);
 }
 
 // ---------------------------------------------------------------------------
@@ -266,100 +346,163 @@ struct Part {
     double top, sum;  // top: NaN where the chunk holds NaN or +inf
 };
 
-// exp(x) for x <= 0, to about 1 ulp: x = n log 2 + r, the series of exp(r) up to r^13
-// (|r| <= 0.347, so the rest is below 2^-57 of it), times 2^n.
-__device__ __forceinline__ double exp_of(double x)
+// Weights: exp((x - top) / T) = 2^(n / 32) 2^(f / 32), where (x - top) (32 / (T log 2)) = n
+// + f with n whole and |f| <= 1/2.  The first factor is a table's entry for n mod 32 (32
+// doubles are each LDS bank once, so that no two lanes meet on one) times a power of
+// two, the second the series of exp(f log 2 / 32) up to f^6 (the rest is below 2^-57 of
+// it).  Relative error 2^-53 times a few, and times |n| / 32 log 2 for what the product's
+// rounding does: 2^-50 for weights of exp(-20), 2^-43 for the least fp64 weights.
+struct Powers {  // LDS
+    double of[32];
+};
+
+__device__ __forceinline__ void make_powers(Powers &p)  // (a barrier has to follow)
 {
-    x = fmax(x, -746.0);  // (whose exponential rounds to 0)
-    const double n = rint(x * 1.4426950408889634);
-    double r = fma(n, -0x1.62e42fefa39efp-1, x);  // log 2 in two parts
-    r = fma(n, -0x1.abc9e3b39803fp-56, r);
-    double p = 1.0 / 6227020800.0;
-    p = fma(p, r, 1.0 / 479001600.0);
-    p = fma(p, r, 1.0 / 39916800.0);
-    p = fma(p, r, 1.0 / 3628800.0);
-    p = fma(p, r, 1.0 / 362880.0);
-    p = fma(p, r, 1.0 / 40320.0);
-    p = fma(p, r, 1.0 / 5040.0);
-    p = fma(p, r, 1.0 / 720.0);
-    p = fma(p, r, 1.0 / 120.0);
-    p = fma(p, r, 1.0 / 24.0);
-    p = fma(p, r, 1.0 / 6.0);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    return ldexp(p, (int)n);
+    if (threadIdx.x < 32) p.of[threadIdx.x] = exp2((double)threadIdx.x / 32.0);
 }
 
-__device__ __forceinline__ double weight_of(float x, double top, double inv_t)
+// scale = 32 / (T log 2)
+__device__ __forceinline__ double power_of(double z, const Powers &p)
 {
-    return exp_of(((double)x - top) * inv_t);
+    z = fmax(z, -746.0 * 32.0 * 1.4426950408889634);  // (whose weight rounds to 0)
+    const double n = rint(z), f = z - n;
+    const int i = (int)n;
+    constexpr double a = 0.693147180559945309417 / 32.0;
+    double q = a * a * a * a * a * a / 720.0;
+    q = fma(q, f, a * a * a * a * a / 120.0);
+    q = fma(q, f, a * a * a * a / 24.0);
+    q = fma(q, f, a * a * a / 6.0);
+    q = fma(q, f, a * a / 2.0);
+    q = fma(q, f, a);
+    const double t = p.of[i & 31];
+    return ldexp(fma(q * f, t, t), i >> 5);
 }
 
-// Sum over the lanes up to and with each.
+__device__ __forceinline__ double weight_of(float x, double top, double scale, const Powers &p)
+{
+    return power_of(((double)x - top) * scale, p);
+}
+
+// The value that DPP control CTRL brings to a lane, 0 where it brings none.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double moved(double v)
+{
+    const u64 b = __builtin_bit_cast(u64, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF,
+                                                    false);
+    return __builtin_bit_cast(double, (u64)hi << 32 | lo);
+}
+
+__device__ __forceinline__ double of_lane(double v, int lane)  // (the same lane for all)
+{
+    const u64 b = __builtin_bit_cast(u64, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+    const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (u64)hi << 32 | lo);
+}
+
+// Sum over the lanes up to and with each: within rows of 16 lanes, then a row's last lane
+// to the next row, then the lower half's last to the upper half.
 __device__ __forceinline__ double prefix(double v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    v += moved<0x111>(v);  // shift right by 1, 2, 4, 8 in the row
+    v += moved<0x112>(v);
+    v += moved<0x114>(v);
+    v += moved<0x118>(v);
+    v += moved<0x142, 0xA>(v);  // lane 15 of a row to the next
+    v += moved<0x143, 0xC>(v);  // lane 31 to the upper half
     return v;
 }
 
-// A choice among 64 shares: the first lane whose prefix exceeds goal, else (rounding, or
-// goal infinite) the last with a share; goal becomes what is left of it, at least 0.
-// some share has to be positive.
-__device__ __forceinline__ int choose(double share, double &goal)
+// Sum over groups of 16 or 32 lanes, in each of their lanes.
+template <int LANES>
+__device__ __forceinline__ double group_sum(double v)
 {
-    const double upto = prefix(share);
+    v += moved<0xB1>(v);   // lane ^ 1
+    v += moved<0x4E>(v);   // lane ^ 2
+    v += moved<0x141>(v);  // the other four of eight
+    v += moved<0x140>(v);  // the other eight of sixteen
+    if constexpr (LANES == 32) v += __shfl_xor(v, 16);
+    return v;
+}
+
+// A choice among 64 shares with the sums `upto`: the first lane whose sum exceeds goal,
+// else (rounding, or goal infinite) the last with a share; goal becomes what is left of
+// it, at least 0.  Some share has to be positive.
+__device__ __forceinline__ int choose(double share, double upto, double &goal)
+{
     const u64 positive = __ballot(share > 0.0);
     const u64 past = __ballot(upto > goal) & positive;
     const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(positive);
-    const double before = at ? __shfl(upto, at - 1) : 0.0;
-    goal = fmax(goal - before, 0.0);
+    goal = fmax(goal - of_lane(upto - share, at), 0.0);
     return at;
 }
 
-// The draws t0, t0 + step.. of a row by one wavefront each.
+// What a row's draws share.
+struct Law {
+    double top, total;  // largest score; sum of the weights
+    double share, upto; // this lane's chunk: its share of the weights, the sum up to it
+    int32_t last;       // first of the last 64 chunks that hold some weight
+    bool is;
+};
+
+__device__ __forceinline__ double chunk_share(const Part *part, int32_t c, int32_t chunks,
+                                              double top, double scale, const Powers &powers)
+{
+    if (c >= chunks) return 0.0;
+    const Part p = part[c];
+    return p.sum > 0.0 ? p.sum * power_of((p.top - top) * scale, powers) : 0.0;
+}
+
+__device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double scale,
+                                      const Powers &powers)
+{
+    const int lane = threadIdx.x & 63;
+    Law law;
+    law.top = -__builtin_inf();
+    bool is = true;
+    for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
+        const double t = c0 + lane < chunks ? part[c0 + lane].top : -__builtin_inf();
+        is = is && t == t;
+        law.top = fmax(law.top, t);
+    }
+    for (int d = 32; d; d >>= 1) law.top = fmax(law.top, __shfl_xor(law.top, d));
+    law.is = !__any(!is) && law.top > -__builtin_inf();
+    law.total = law.share = law.upto = 0.0;
+    law.last = 0;
+    if (law.is)
+        for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
+            law.share = chunk_share(part, c0 + lane, chunks, law.top, scale, powers);
+            law.upto = prefix(law.share);
+            law.total += of_lane(law.upto, 63);
+            if (__any(law.share > 0.0)) law.last = c0;
+        }
+    return law;
+}
+
+constexpr int kListed = 8;  // words of the document that a lane keeps
+
+// The draws t0, t0 + stride .. of a row by one wavefront, one after another.
 template <typename T>
 __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, const RowRules &r,
-                                           double inv_t, int32_t chunks, const Part *part,
-                                           const double *blocks, int32_t t0, int32_t step,
-                                           int32_t draws, int64_t d0, const double *__restrict__ u,
-                                           uint64_t seed, uint32_t philox_step, int64_t draw0,
+                                           double scale, int32_t chunks, const Part *part,
+                                           const double *blocks, const Powers &powers, int32_t t0,
+                                           int32_t stride, int32_t draws, int64_t d0,
+                                           const double *__restrict__ u, uint64_t seed,
+                                           uint32_t step, int64_t draw0,
                                            int32_t *__restrict__ word, float *__restrict__ logp)
 {
     const int lane = threadIdx.x & 63;
-    // the row's largest score and the sum of its weights
-    double top = -__builtin_inf();
-    bool law = true;
-    for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
-        const double t = c0 + lane < chunks ? part[c0 + lane].top : -__builtin_inf();
-        law = law && t == t;
-        top = fmax(top, t);
-    }
-    for (int d = 32; d; d >>= 1) top = fmax(top, __shfl_xor(top, d));
-    law = !__any(!law) && top > -__builtin_inf();
-    auto share_of = [&](int32_t c) {
-        if (c >= chunks) return 0.0;
-        const Part p = part[c];
-        return p.sum > 0.0 ? p.sum * exp_of((p.top - top) * inv_t) : 0.0;
-    };
-    double total = 0.0, share = 0.0;
-    int32_t last = 0;  // the last 64 chunks that hold some weight
-    if (law) {
-        for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
-            share = share_of(c0 + lane);
-            total += __shfl(prefix(share), 63);
-            if (__any(share > 0.0)) last = c0;
-        }
-    }
-    const double log_total = log(total);
-    for (int32_t t = t0; t < draws; t += step) {
+    int32_t listed[kListed];
+#pragma unroll
+    for (int i = 0; i < kListed; ++i)
+        listed[i] = i * 64 + lane < r.n_words ? r.words[i * 64 + lane] : -1;
+    const Law law = law_of(part, chunks, scale, powers);
+    const double log_total = law.is ? log(law.total) : 0.0;
+    for (int32_t t = t0; t < draws; t += stride) {
         const int64_t d = d0 + t;
-        if (!law) {
+        if (!law.is) {
             if (lane == 0) {
                 word[d] = -1;
                 logp[d] = __builtin_nanf("");
@@ -367,52 +510,61 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
             continue;
         }
         const double uniform =
-            u ? u[d]
-              : (double)philox_x0(seed, (uint64_t)(draw0 + d), philox_step, kPurposeWord) * 0x1p-32;
+            u ? u[d] : (double)philox_x0(seed, (uint64_t)(draw0 + d), step, kPurposeWord) * 0x1p-32;
         // (NaN, and 1 or more: the last word with weight)
-        double goal = uniform * total < total ? fmax(uniform * total, 0.0) : __builtin_inf();
-        // 64 chunks at a time, the ones whose shares exceed what is left of the goal
+        double goal = uniform * law.total < law.total ? fmax(uniform * law.total, 0.0)
+                                                      : __builtin_inf();
         int32_t c0 = 0;
+        double share = law.share, upto = law.upto;
         if (chunks > 64) {
-            for (; c0 < last; c0 += 64) {
-                share = share_of(c0 + lane);
-                const double sum = __shfl(prefix(share), 63);
-                if (sum > goal) break;
+            // 64 chunks at a time: the first whose sum exceeds what is left of the goal
+            for (;; c0 += 64) {
+                share = chunk_share(part, c0 + lane, chunks, law.top, scale, powers);
+                upto = prefix(share);
+                const double sum = of_lane(upto, 63);
+                if (sum > goal || c0 >= law.last) break;
                 goal -= sum;
             }
-            share = share_of(c0 + lane);
         }
-        const int32_t c = c0 + choose(share, goal);
+        const int32_t c = c0 + choose(share, upto, goal);
         const double own = part[c].top;
-        goal = goal / exp_of((own - top) * inv_t);
-        const int b = choose(blocks[(int64_t)c * kBlocks + lane], goal);
+        goal = goal / power_of((own - law.top) * scale, powers);
+        share = blocks[(int64_t)c * kBlocks + lane];
+        const int b = choose(share, prefix(share), goal);
         // the block's words, two a lane
-        const int64_t w = (int64_t)c * kDrawChunk + b * kBlockWords + 2 * lane;
+        const int64_t b0 = (int64_t)c * kDrawChunk + b * kBlockWords, w = b0 + 2 * lane;
         float s[2];
         int32_t n[2] = {0, 0};
-        for (int64_t i = 0; i < r.n_words; i += 64) {
-            const int64_t at =
-                i + lane < r.n_words ? (int64_t)r.words[i + lane] - (w - 2 * lane) : -1;
+        auto count = [&](int32_t entry) {
+            const int64_t at = (int64_t)entry - b0;
             u64 hits = __ballot(at >= 0 && at < kBlockWords);
             while (hits) {
-                const int from = __builtin_ctzll(hits);
+                const int a = __builtin_amdgcn_readlane((int)at, __builtin_ctzll(hits));
                 hits &= hits - 1;
-                const int a = __shfl((int)at, from);
                 n[0] += a == 2 * lane;
                 n[1] += a == 2 * lane + 1;
             }
+        };
+        if (r.n_words > 0) {
+#pragma unroll
+            for (int i = 0; i < kListed; ++i) count(listed[i]);
+            for (int64_t i = kListed * 64; i < r.n_words; i += 64)
+                count(i + lane < r.n_words ? r.words[i + lane] : -1);
         }
         double y[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             s[i] = w + i < V ? ruled(r, (float)x[w + i], w + i, n[i]) : -__builtin_inff();
-            y[i] = weight_of(s[i], own, inv_t);
+            y[i] = weight_of(s[i], own, scale, powers);
         }
-        const int l = choose(y[0] + y[1], goal);
-        const bool second = !(y[0] > goal) && y[1] > 0.0;
+        share = y[0] + y[1];
+        const int l = choose(share, prefix(share), goal);
         if (lane == l) {
+            const bool second = !(y[0] > goal) && y[1] > 0.0;
             word[d] = (int32_t)(w + second);
-            logp[d] = (float)(((double)(second ? s[1] : s[0]) - top) * inv_t - log_total);
+            logp[d] = (float)(((double)(second ? s[1] : s[0]) - law.top) * scale *
+                                  (0.693147180559945309417 / 32.0) -
+                              log_total);
         }
     }
 }
@@ -421,7 +573,7 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
 // drawn from at once.
 template <typename T>
 __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
-    const T *__restrict__ x, int64_t ld, int64_t V, int32_t chunks, spdp_rules rules, double inv_t,
+    const T *__restrict__ x, int64_t ld, int64_t V, int32_t chunks, spdp_rules rules, double scale,
     Part *__restrict__ part, double *__restrict__ blocks, int32_t draws,
     const double *__restrict__ u, uint64_t seed, uint32_t step, int64_t draw0,
     int32_t *__restrict__ word, float *__restrict__ logp)
@@ -432,6 +584,8 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
     __shared__ float wave_top[kDrawThreads / 64];
     __shared__ double sum_of[kBlocks];
     __shared__ Part own;
+    __shared__ Powers powers;
+    make_powers(powers);
     const int64_t row = blockIdx.x / (uint32_t)chunks;
     const int32_t chunk = blockIdx.x % (uint32_t)chunks;
     const int64_t w0 = (int64_t)chunk * C::kWords;
@@ -462,16 +616,15 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
         double s = 0.0;
         if (some) {
 #pragma unroll
-            for (int i = 0; i < C::N; ++i) s += weight_of(v[k][i], top, inv_t);
+            for (int i = 0; i < C::N; ++i) s += weight_of(v[k][i], top, scale, powers);
         }
-#pragma unroll
-        for (int d = 1; d < kLanes; d *= 2) s += __shfl_xor(s, d);
+        s = group_sum<kLanes>(s);
         const int b = C::at(k) / kBlockWords;
         if (lane % kLanes == 0) sum_of[b] = s;
     }
     __syncthreads();
     if (wave == 0) {
-        const double s = sum_of[lane], sum = __shfl(prefix(s), 63);
+        const double s = sum_of[lane], sum = of_lane(prefix(s), 63);
         if (lane == 0) own = Part{law ? (double)top : __builtin_nan(""), sum};
         if (chunks > 1) {
             blocks[(int64_t)blockIdx.x * kBlocks + lane] = s;
@@ -480,14 +633,14 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
     }
     if (chunks > 1) return;
     __syncthreads();
-    draw_words(x + row * ld, V, r, inv_t, 1, &own, sum_of, wave, kDrawThreads / 64, draws,
+    draw_words(x + row * ld, V, r, scale, 1, &own, sum_of, powers, wave, kDrawThreads / 64, draws,
                row * draws, u, seed, step, draw0, word, logp);
 }
 
 // `share` workgroups of four wavefronts per row.
 template <typename T>
 __global__ void __launch_bounds__(256) k_draw(const T *__restrict__ x, int64_t ld, int64_t V,
-                                              int32_t chunks, spdp_rules rules, double inv_t,
+                                              int32_t chunks, spdp_rules rules, double scale,
                                               const Part *__restrict__ part,
                                               const double *__restrict__ blocks, int32_t share,
                                               int32_t draws, const double *__restrict__ u,
@@ -497,11 +650,14 @@ __global__ void __launch_bounds__(256) k_draw(const T *__restrict__ x, int64_t l
 {
     const int64_t row = blockIdx.x / (uint32_t)share;
     const int32_t t0 = (int32_t)(blockIdx.x % (uint32_t)share) * 4 + (threadIdx.x >> 6);
+    __shared__ Powers powers;
+    make_powers(powers);
+    __syncthreads();
     if (t0 >= draws) return;
     const RowRules r = row_rules(rules, row);
-    draw_words(x + row * ld, V, r, inv_t, chunks, part + row * chunks,
-               blocks + row * chunks * kBlocks, t0, 4 * share, draws, row * draws, u, seed, step,
-               draw0, word, logp);
+    draw_words(x + row * ld, V, r, scale, chunks, part + row * chunks,
+               blocks + row * chunks * kBlocks, powers, t0, 4 * share, draws, row * draws, u, seed,
+               step, draw0, word, logp);
 }
 
 // launch(value of the scores' type, grid), and its error
@@ -517,13 +673,13 @@ hipError_t by_type(int32_t type, int64_t blocks, F launch)
 
 int64_t chunks_of(int64_t V, int64_t words) { return (V + words - 1) / words; }
 
-// Parts of a row for the best words: as many as chunks while the rows alone leave compute
-// units idle, else chunks one after another in a workgroup (few scores of the later ones
-// pass the bound), with about six workgroups for a compute unit.
+// Parts of a row for the best words, of even length: as many as chunks while the rows alone
+// leave compute units idle, else several chunks one after another in a workgroup (few
+// scores of the later ones pass the bound).
 constexpr int64_t kTopBlocks = 1536;
 
 struct TopShape {
-    int64_t parts, per;
+    int64_t parts, words;
 };
 
 TopShape top_shape(int64_t rows, int64_t V)
@@ -531,8 +687,8 @@ TopShape top_shape(int64_t rows, int64_t V)
     const int64_t chunks = chunks_of(V, kTopThreads * 16);
     int64_t parts = rows > 0 ? (kTopBlocks + rows - 1) / rows : 1;
     parts = parts > chunks ? chunks : parts;
-    const int64_t per = (chunks + parts - 1) / parts;
-    return TopShape{(chunks + per - 1) / per, per};
+    const int64_t words = ((V + parts - 1) / parts + 31) / 32 * 32;  // (masks' words)
+    return TopShape{(V + words - 1) / words, words};
 }
 
 int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
@@ -580,7 +736,7 @@ hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int
     hipError_t e = by_type(type, rows * s.parts, [&](auto t, dim3 grid) {
         using T = decltype(t);
         hipLaunchKernelGGL(k_top_part<T>, grid, dim3(kTopThreads), 0, st, (const T *)x, ld, V,
-                           (int32_t)s.parts, (int32_t)s.per, rules, k, best, word, value);
+                           (int32_t)s.parts, s.words, rules, k, best, word, value);
     });
     if (e != hipSuccess || s.parts == 1) return e;
     hipLaunchKernelGGL(k_top_join, dim3((unsigned)rows), dim3(kTopThreads), 0, st, best,
@@ -595,14 +751,14 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
 {
     if (rows == 0 || draws == 0) return hipSuccess;
     const int64_t chunks = chunks_of(V, kDrawChunk);
-    const double inv_t = 1.0 / temperature;
+    const double scale = 32.0 * 1.44269504088896340736 / temperature;
     Part *part = static_cast<Part *>(work);
     double *blocks = reinterpret_cast<double *>(static_cast<char *>(work) +
                                                 draw_parts_bytes(rows, chunks));
     hipError_t e = by_type(type, rows * chunks, [&](auto t, dim3 grid) {
         using T = decltype(t);
         hipLaunchKernelGGL(k_draw_parts<T>, grid, dim3(kDrawThreads), 0, st, (const T *)x, ld, V,
-                           (int32_t)chunks, rules, inv_t, part, blocks, draws, u, seed, step, draw0,
+                           (int32_t)chunks, rules, scale, part, blocks, draws, u, seed, step, draw0,
                            word, logp);
     });
     if (e != hipSuccess || chunks == 1) return e;
@@ -613,7 +769,7 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
     return by_type(type, rows * share, [&](auto t, dim3 grid) {
         using T = decltype(t);
         hipLaunchKernelGGL(k_draw<T>, grid, dim3(256), 0, st, (const T *)x, ld, V, (int32_t)chunks,
-                           rules, inv_t, part, blocks, (int32_t)share, draws, u, seed, step, draw0,
+                           rules, scale, part, blocks, (int32_t)share, draws, u, seed, step, draw0,
                            word, logp);
     });
 }
