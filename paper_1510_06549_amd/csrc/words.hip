@@ -66,16 +66,43 @@ constexpr int kKeys = 2048;  // kept at a time in LDS
 
 struct Kept {  // LDS
     u64 key[kKeys];
-    int in_wave[2][kTopWaves];
-    int n;
+    int in_wave[2][3][kTopWaves];
 };
 
-// Cuts the n keys (k < n <= kKeys) down to the k largest, kept.n of them in any order (less
-// than k where there are not so many but 0), and returns a bound that only they reach:
-// the largest that k keys reach, found bit by bit from the first bit that not all keys have
-// alike until exactly k reach it.  All threads call it, behind a barrier; there is one
-// before it returns.
-__device__ __forceinline__ u64 cut_keys(Kept &kept, int n, int k)
+// Sum over the lanes up to and with each.
+__device__ __forceinline__ int prefix(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // shift right by 1, 2, 4,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);  // 8 in rows of 16 lanes,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 to the next row,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to the upper half
+    return v;
+}
+
+// Places for `mine` keys of each thread, in the threads' order: the thread's first place
+// behind `before`, and in total how many places there are.  All threads call it; `slot` may
+// be used again behind the next barrier but one.
+__device__ __forceinline__ int places(int mine, int before, int (&slot)[kTopWaves], int &total)
+{
+    const int upto = prefix(mine), wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) slot[wave] = upto;
+    __syncthreads();
+    total = 0;
+    for (int i = 0; i < kTopWaves; ++i) {
+        if (i < wave) before += slot[i];
+        total += slot[i];
+    }
+    return before + upto - mine;
+}
+
+// Cuts the n keys (k < n <= kKeys) down to the k largest, in any order, and returns how many
+// there are (less than k where there are not so many but 0); least is a bound that only
+// they reach: the largest that k keys reach, found two bits at a time, over the bits that
+// not all keys have alike, until exactly k reach it.  All threads call it, behind a
+// barrier; there is one before it returns.
+__device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
 {
     constexpr int kPer = kKeys / kTopThreads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -104,35 +131,42 @@ __device__ __forceinline__ u64 cut_keys(Kept &kept, int n, int k)
         any |= kept.key[2 * i];
         all &= kept.key[2 * i + 1];
     }
-    const u64 differ = any ^ all;
-    u64 bit = differ ? 1ull << (63 - __builtin_clzll(differ)) : 0;
-    u64 bound = differ ? all & ~(2 * bit - 1) : all;
-    for (int turn = 0; bit; bit >>= 1, turn ^= 1) {
-        const u64 t = bound | bit;
-        int reach = 0;
+    u64 differ = any ^ all, bound = all;
+    for (int turn = 0; differ; turn ^= 1) {
+        const u64 high = 1ull << (63 - __builtin_clzll(differ)), rest = differ ^ high;
+        const u64 low = rest ? 1ull << (63 - __builtin_clzll(rest)) : 0;
+        const u64 t[3] = {bound | high | low, bound | high, bound | low};
+        int reach[3] = {0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) reach += __builtin_popcountll(__ballot(key[i] >= t));
-        if (lane == 0) kept.in_wave[turn][wave] = reach;
+        for (int i = 0; i < kPer; ++i) {
+            if (i * kTopThreads >= n) break;
+#pragma unroll
+            for (int j = 0; j < 3; ++j) reach[j] += __builtin_popcountll(__ballot(key[i] >= t[j]));
+        }
+        if (lane == 0)
+            for (int j = 0; j < 3; ++j) kept.in_wave[turn][j][wave] = reach[j];
         __syncthreads();
-        reach = 0;
-        for (int i = 0; i < kTopWaves; ++i) reach += kept.in_wave[turn][i];
-        if (reach >= k) bound = t;
-        if (reach == k) break;
+        for (int j = 0; j < 3; ++j) {
+            reach[j] = 0;
+            for (int i = 0; i < kTopWaves; ++i) reach[j] += kept.in_wave[turn][j][i];
+        }
+        const int j = reach[0] >= k ? 0 : reach[1] >= k ? 1 : low && reach[2] >= k ? 2 : 3;
+        if (j < 3) bound = t[j];
+        if (j < 3 && reach[j] == k) break;
+        differ = rest ^ low;
     }
     bound = bound ? bound : 1;
-    if (threadIdx.x == 0) kept.n = 0;
-    __syncthreads();
     int mine = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) mine += key[i] >= bound;
-    if (mine) {
-        int to = atomicAdd(&kept.n, mine);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (key[i] >= bound) kept.key[to++] = key[i];
-    }
     __syncthreads();
-    return bound;
+    int total, to = places(mine, 0, kept.in_wave[0][0], total);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (key[i] >= bound) kept.key[to++] = key[i];
+    __syncthreads();
+    least = bound;
+    return total;
 }
 
 // Calls put(rank, key) for the k largest of the n keys, n <= kTopThreads: a key's rank is
@@ -162,8 +196,8 @@ __device__ __forceinline__ void put_top(u64 key, int32_t *word, float *value)
 // the first chunk few scores pass.  Where the collection would overflow (many ties), it
 // is cut down to its k best, again and again.
 template <typename T>
-__global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ x, int64_t ld,
-                                                          int64_t V, int32_t parts, int64_t words,
+__global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict__ x, int64_t ld,
+                                                             int64_t V, int32_t parts, int64_t words,
                                                           spdp_rules rules, int32_t k,
                                                           u64 *__restrict__ best,
                                                           int32_t *__restrict__ word,
@@ -173,7 +207,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
     __shared__ typename C::Listed listed;
     __shared__ Kept kept;
     __shared__ uint32_t wave_least[kTopWaves];
-    __shared__ int passing;
+    __shared__ int wave_pass[kTopWaves];
     const int64_t row = blockIdx.x / (uint32_t)parts;
     const int64_t first = (int64_t)(blockIdx.x % (uint32_t)parts) * words;
     const int64_t end = first + words < V ? first + words : V;
@@ -188,7 +222,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
     int group = 1;
     while (group < kTopThreads && (threads + 2 * group - 1) / (2 * group) >= k) group *= 2;
     const bool grouped = threads >= k, holds = (int)threadIdx.x < threads;
-    if (threadIdx.x == 0) kept.n = 0;
+    int n = 0;           // keys kept
     uint32_t mine = 0;   // largest order that this thread has seen
     u64 bound = 1;       // keys below are not among the k best
     for (int64_t w0 = first; w0 < end; w0 += C::kWords) {
@@ -218,7 +252,6 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
             g = o < g ? o : g;
         }
         if ((threadIdx.x & 63) == 0) wave_least[threadIdx.x >> 6] = g;
-        if (threadIdx.x == 0) passing = 0;
         __syncthreads();
         if (grouped) {
             const uint32_t *w = wave_least;
@@ -235,13 +268,9 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
 #pragma unroll
             for (int i = 0; i < C::N; ++i)
                 pass |= (uint32_t)(order[u][i] >= low) << (u * C::N + i);
-        if (pass) atomicAdd(&passing, __builtin_popcount(pass));
-        __syncthreads();
-        const int room = kKeys - kept.n - passing;
-        __syncthreads();
-        if (room >= 0) {
+        int passing, to = places(__builtin_popcount(pass), n, wave_pass, passing);
+        if (n + passing <= kKeys) {
             if (pass) {
-                int to = atomicAdd(&kept.n, __builtin_popcount(pass));
 #pragma unroll
                 for (int u = 0; u < C::U; ++u)
 #pragma unroll
@@ -249,6 +278,7 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
                         if (pass >> (u * C::N + i) & 1u)
                             kept.key[to++] = key_of(order[u][i], w0 + C::at(u) + i);
             }
+            n += passing;
             __syncthreads();
             continue;
         }
@@ -257,26 +287,30 @@ __global__ void __launch_bounds__(kTopThreads) k_top_part(const T *__restrict__ 
         for (int u = 0; u < C::U; ++u)
 #pragma unroll
             for (int i = 0; i < C::N; i += 4) {
-                const int m = kept.n;
-                __syncthreads();  // (everybody has read it)
-                if (m > kKeys / 2) {
-                    const u64 b = cut_keys(kept, m, k);
-                    bound = b > bound ? b : bound;
+                __syncthreads();
+                if (n > kKeys / 2) {
+                    u64 least;
+                    n = cut_keys(kept, n, k, least);
+                    bound = least > bound ? least : bound;
                 }
+                u64 key[4];
+                int more = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const u64 key = key_of(order[u][i + e], w0 + C::at(u) + i + e);
-                    if (key >= bound) kept.key[atomicAdd(&kept.n, 1)] = key;
+                    key[e] = key_of(order[u][i + e], w0 + C::at(u) + i + e);
+                    more += key[e] >= bound;
                 }
-                __syncthreads();
+                int at = places(more, n, wave_pass, passing);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (key[e] >= bound) kept.key[at++] = key[e];
+                n += passing;
             }
+        __syncthreads();
     }
-    __syncthreads();
-    int n = kept.n;
-    __syncthreads();
     if (n > kTopThreads) {
-        cut_keys(kept, n, k);
-        n = k;
+        u64 least;
+        n = cut_keys(kept, n, k, least);
     }
     word += row * k;
     value += row * k;
@@ -307,8 +341,8 @@ __global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict_
         have += take;
         __syncthreads();
         if (have > kTopThreads) {
-            cut_keys(kept, have, k);
-            have = kept.n;
+            u64 least;
+            have = cut_keys(kept, have, k, least);
         }
     }
     word += row * k;
@@ -675,8 +709,9 @@ int64_t chunks_of(int64_t V, int64_t words) { return (V + words - 1) / words; }
 
 // Parts of a row for the best words, of even length: as many as chunks while the rows alone
 // leave compute units idle, else several chunks one after another in a workgroup (few
-// scores of the later ones pass the bound).
-constexpr int64_t kTopBlocks = 1536;
+// scores of the later ones pass the bound), all parts of all rows at once on the chip
+// (four workgroups a compute unit; 400 rows of 50 000: two parts 58 us, three 71, four 66).
+constexpr int64_t kTopBlocks = 1024;
 
 struct TopShape {
     int64_t parts, words;
@@ -685,8 +720,10 @@ struct TopShape {
 TopShape top_shape(int64_t rows, int64_t V)
 {
     const int64_t chunks = chunks_of(V, kTopThreads * 16);
-    int64_t parts = rows > 0 ? (kTopBlocks + rows - 1) / rows : 1;
+    int64_t parts = rows > 0 && rows < kTopBlocks ? kTopBlocks / rows : 1;
     parts = parts > chunks ? chunks : parts;
+    const int64_t per = (chunks + parts - 1) / parts;  // chunks of a part
+    parts = (chunks + per - 1) / per;
     const int64_t words = ((V + parts - 1) / parts + 31) / 32 * 32;  // (masks' words)
     return TopShape{(V + words - 1) / words, words};
 }
