@@ -372,8 +372,8 @@ __global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict_
 // chunk's 64, the word among its block's 128 scores, each by a prefix sum over the
 // lanes.
 // ---------------------------------------------------------------------------
-constexpr int kDrawThreads = 512;
-constexpr int kDrawChunk = kDrawThreads * 16;
+constexpr int kDrawThreads = 512, kDrawPer = 16;
+constexpr int kDrawChunk = kDrawThreads * kDrawPer;
 constexpr int kBlocks = 64, kBlockWords = kDrawChunk / kBlocks;
 
 struct Part {
@@ -383,9 +383,9 @@ struct Part {
 // Weights: exp((x - top) / T) = 2^(n / 32) 2^(f / 32), where (x - top) (32 / (T log 2)) = n
 // + f with n whole and |f| <= 1/2.  The first factor is a table's entry for n mod 32 (32
 // doubles are each LDS bank once, so that no two lanes meet on one) times a power of
-// two, the second the series of exp(f log 2 / 32) up to f^6 (the rest is below 2^-57 of
-// it).  Relative error 2^-53 times a few, and times |n| / 32 log 2 for what the product's
-// rounding does: 2^-50 for weights of exp(-20), 2^-43 for the least fp64 weights.
+// two, the second the series of exp(f log 2 / 32) up to f^5 (the rest is below 2^-48 of
+// it).  The product's rounding adds 2^-53 |n| / 32 log 2: 2^-49 for weights of exp(-20),
+// 2^-43 for the least fp64 weights.
 struct Powers {  // LDS
     double of[32];
 };
@@ -398,12 +398,15 @@ __device__ __forceinline__ void make_powers(Powers &p)  // (a barrier has to fol
 // scale = 32 / (T log 2)
 __device__ __forceinline__ double power_of(double z, const Powers &p)
 {
-    z = fmax(z, -746.0 * 32.0 * 1.4426950408889634);  // (whose weight rounds to 0)
+    // z <= 0: its magnitude is cut to 34 440 and a little, whose weight rounds to 0 (a comparison
+    // of the high words as they are, one instruction; -inf and -0 come out right)
+    const u64 bits = __builtin_bit_cast(u64, z);
+    const uint32_t high = min((uint32_t)(bits >> 32), 0xC0E0D100u);
+    z = __builtin_bit_cast(double, (u64)high << 32 | (uint32_t)bits);
     const double n = rint(z), f = z - n;
     const int i = (int)n;
     constexpr double a = 0.693147180559945309417 / 32.0;
-    double q = a * a * a * a * a * a / 720.0;
-    q = fma(q, f, a * a * a * a * a / 120.0);
+    double q = a * a * a * a * a / 120.0;
     q = fma(q, f, a * a * a * a / 24.0);
     q = fma(q, f, a * a * a / 6.0);
     q = fma(q, f, a * a / 2.0);
@@ -476,39 +479,49 @@ __device__ __forceinline__ int choose(double share, double upto, double &goal)
 // What a row's draws share.
 struct Law {
     double top, total;  // largest score; sum of the weights
-    double share, upto; // this lane's chunk: its share of the weights, the sum up to it
+    double share, upto; // this lane's chunk: its share of the weights, the sum up to it,
+    double own, inverse; // its largest score, and by what its own weights exceed their share
     int32_t last;       // first of the last 64 chunks that hold some weight
     bool is;
 };
 
-__device__ __forceinline__ double chunk_share(const Part *part, int32_t c, int32_t chunks,
-                                              double top, double scale, const Powers &powers)
+// This lane's chunk.
+__device__ __forceinline__ void lane_chunk(Law &law, const Part *part, int32_t c, int32_t chunks,
+                                           double scale, const Powers &powers)
 {
-    if (c >= chunks) return 0.0;
-    const Part p = part[c];
-    return p.sum > 0.0 ? p.sum * power_of((p.top - top) * scale, powers) : 0.0;
+    law.share = 0.0;
+    law.own = law.top;
+    law.inverse = 1.0;
+    if (c < chunks) {
+        const Part p = part[c];
+        if (p.sum > 0.0) {
+            const double w = power_of((p.top - law.top) * scale, powers);
+            law.share = p.sum * w;
+            law.own = p.top;
+            law.inverse = 1.0 / w;
+        }
+    }
+    law.upto = prefix(law.share);
 }
 
 __device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double scale,
                                       const Powers &powers)
 {
     const int lane = threadIdx.x & 63;
-    Law law;
-    law.top = -__builtin_inf();
+    Law law{};
+    float top = -__builtin_inff();
     bool is = true;
     for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
-        const double t = c0 + lane < chunks ? part[c0 + lane].top : -__builtin_inf();
+        const float t = c0 + lane < chunks ? (float)part[c0 + lane].top : -__builtin_inff();
         is = is && t == t;
-        law.top = fmax(law.top, t);
+        top = fmaxf(top, t);
     }
-    for (int d = 32; d; d >>= 1) law.top = fmax(law.top, __shfl_xor(law.top, d));
-    law.is = !__any(!is) && law.top > -__builtin_inf();
-    law.total = law.share = law.upto = 0.0;
-    law.last = 0;
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    law.top = top;
+    law.is = !__any(!is) && top > -__builtin_inff();
     if (law.is)
         for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
-            law.share = chunk_share(part, c0 + lane, chunks, law.top, scale, powers);
-            law.upto = prefix(law.share);
+            lane_chunk(law, part, c0 + lane, chunks, scale, powers);
             law.total += of_lane(law.upto, 63);
             if (__any(law.share > 0.0)) law.last = c0;
         }
@@ -517,14 +530,14 @@ __device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double s
 
 constexpr int kListed = 8;  // words of the document that a lane keeps
 
-// The draws t0, t0 + stride .. of a row by one wavefront, one after another.
+// `count` draws from d0 on of a row by one wavefront, a lane for each uniform and its
+// answer, one after another.
 template <typename T>
 __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, const RowRules &r,
                                            double scale, int32_t chunks, const Part *part,
-                                           const double *blocks, const Powers &powers, int32_t t0,
-                                           int32_t stride, int32_t draws, int64_t d0,
-                                           const double *__restrict__ u, uint64_t seed,
-                                           uint32_t step, int64_t draw0,
+                                           const double *blocks, const Powers &powers, int64_t d0,
+                                           int32_t count, const double *__restrict__ u,
+                                           uint64_t seed, uint32_t step, int64_t draw0,
                                            int32_t *__restrict__ word, float *__restrict__ logp)
 {
     const int lane = threadIdx.x & 63;
@@ -532,73 +545,95 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
 #pragma unroll
     for (int i = 0; i < kListed; ++i)
         listed[i] = i * 64 + lane < r.n_words ? r.words[i * 64 + lane] : -1;
-    const Law law = law_of(part, chunks, scale, powers);
+    Law law = law_of(part, chunks, scale, powers);
     const double log_total = law.is ? log(law.total) : 0.0;
-    for (int32_t t = t0; t < draws; t += stride) {
-        const int64_t d = d0 + t;
-        if (!law.is) {
-            if (lane == 0) {
-                word[d] = -1;
-                logp[d] = __builtin_nanf("");
-            }
-            continue;
-        }
-        const double uniform =
-            u ? u[d] : (double)philox_x0(seed, (uint64_t)(draw0 + d), step, kPurposeWord) * 0x1p-32;
-        // (NaN, and 1 or more: the last word with weight)
-        double goal = uniform * law.total < law.total ? fmax(uniform * law.total, 0.0)
-                                                      : __builtin_inf();
-        int32_t c0 = 0;
-        double share = law.share, upto = law.upto;
-        if (chunks > 64) {
-            // 64 chunks at a time: the first whose sum exceeds what is left of the goal
-            for (;; c0 += 64) {
-                share = chunk_share(part, c0 + lane, chunks, law.top, scale, powers);
-                upto = prefix(share);
-                const double sum = of_lane(upto, 63);
-                if (sum > goal || c0 >= law.last) break;
-                goal -= sum;
-            }
-        }
-        const int32_t c = c0 + choose(share, upto, goal);
-        const double own = part[c].top;
-        goal = goal / power_of((own - law.top) * scale, powers);
-        share = blocks[(int64_t)c * kBlocks + lane];
-        const int b = choose(share, prefix(share), goal);
-        // the block's words, two a lane
-        const int64_t b0 = (int64_t)c * kDrawChunk + b * kBlockWords, w = b0 + 2 * lane;
-        float s[2];
-        int32_t n[2] = {0, 0};
-        auto count = [&](int32_t entry) {
-            const int64_t at = (int64_t)entry - b0;
-            u64 hits = __ballot(at >= 0 && at < kBlockWords);
-            while (hits) {
-                const int a = __builtin_amdgcn_readlane((int)at, __builtin_ctzll(hits));
-                hits &= hits - 1;
-                n[0] += a == 2 * lane;
-                n[1] += a == 2 * lane + 1;
-            }
-        };
-        if (r.n_words > 0) {
+    for (int32_t t0 = 0; t0 < count; t0 += 64) {
+        const int64_t d = d0 + t0 + lane;
+        const bool here = t0 + lane < count;
+        int32_t my_word = -1;
+        float my_logp = __builtin_nanf("");
+        if (law.is) {
+            const double uniform =
+                !here ? 0.0
+                : u   ? u[d]
+                      : (double)philox_x0(seed, (uint64_t)(draw0 + d), step, kPurposeWord) * 0x1p-32;
+            // (NaN, and 1 or more: the last word with weight)
+            const double my_goal = uniform * law.total < law.total
+                                       ? fmax(uniform * law.total, 0.0)
+                                       : __builtin_inf();
+            const int32_t many = count - t0 < 64 ? count - t0 : 64;
+            for (int32_t t = 0; t < many; ++t) {
+                double goal = of_lane(my_goal, t);
+                int32_t c0 = 0;
+                if (chunks > 64) {
+                    // 64 chunks at a time: the first whose sum exceeds what is left
+                    for (;; c0 += 64) {
+                        lane_chunk(law, part, c0 + lane, chunks, scale, powers);
+                        const double sum = of_lane(law.upto, 63);
+                        if (sum > goal || c0 >= law.last) break;
+                        goal -= sum;
+                    }
+                }
+                const int at = choose(law.share, law.upto, goal);
+                const double own = of_lane(law.own, at), inverse = of_lane(law.inverse, at);
+                goal = goal > 0.0 ? goal * inverse : 0.0;
+                const double share = blocks[(int64_t)(c0 + at) * kBlocks + lane];
+                const int b = choose(share, prefix(share), goal);
+                // the block's words, two a lane: everything that is read of them at once
+                const int64_t b0 = (int64_t)(c0 + at) * kDrawChunk + b * kBlockWords;
+                const int64_t w = b0 + 2 * lane;
+                float s[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
+                uint32_t allowed = 3;
 #pragma unroll
-            for (int i = 0; i < kListed; ++i) count(listed[i]);
-            for (int64_t i = kListed * 64; i < r.n_words; i += 64)
-                count(i + lane < r.n_words ? r.words[i + lane] : -1);
-        }
-        double y[2];
+                for (int i = 0; i < 2; ++i)
+                    if (w + i < V) {
+                        s[i] = (float)x[w + i];
+                        if (r.bias) bias[i] = r.bias[w + i];
+                    }
+                if (r.mask && w < V) allowed = r.mask[w >> 5] >> (w & 31);
+                int32_t n[2] = {0, 0};
+                auto tally = [&](int32_t entry) {
+                    const uint32_t a = (uint32_t)entry - (uint32_t)b0;
+                    u64 hits = __ballot(a < (uint32_t)kBlockWords && entry >= 0);
+                    while (hits) {
+                        const int h = __builtin_amdgcn_readlane((int)a, __builtin_ctzll(hits));
+                        hits &= hits - 1;
+                        n[0] += h == 2 * lane;
+                        n[1] += h == 2 * lane + 1;
+                    }
+                };
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            s[i] = w + i < V ? ruled(r, (float)x[w + i], w + i, n[i]) : -__builtin_inff();
-            y[i] = weight_of(s[i], own, scale, powers);
-        }
-        share = y[0] + y[1];
-        const int l = choose(share, prefix(share), goal);
-        if (lane == l) {
-            const bool second = !(y[0] > goal) && y[1] > 0.0;
-            word[d] = (int32_t)(w + second);
-            logp[d] = (float)(((double)(second ? s[1] : s[0]) - law.top) * scale *
+                for (int i = 0; i < kListed; ++i)
+                    if (i * 64 < r.n_words) tally(listed[i]);
+                for (int64_t i = kListed * 64; i < r.n_words; i += 64)
+                    tally(i + lane < r.n_words ? r.words[i + lane] : -1);
+                double y[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (n[i] > 0) s[i] = penalised(r, s[i], n[i]);
+                    if (r.bias) s[i] = s[i] + bias[i];
+                    s[i] = (allowed >> i & 1u) && w + i < V ? s[i] : -__builtin_inff();
+                    y[i] = weight_of(s[i], own, scale, powers);
+                }
+                const double both = y[0] + y[1];
+                const int l = choose(both, prefix(both), goal);
+                const bool second = !(y[0] > goal) && y[1] > 0.0;
+                const int32_t got = __builtin_amdgcn_readlane((int)(w + second), l);
+                const float score = __builtin_bit_cast(
+                    float, __builtin_amdgcn_readlane(
+                               __builtin_bit_cast(int, second ? s[1] : s[0]), l));
+                if (lane == t) {
+                    my_word = got;
+                    my_logp = score;
+                }
+            }
+            my_logp = (float)(((double)my_logp - law.top) * scale *
                                   (0.693147180559945309417 / 32.0) -
                               log_total);
+        }
+        if (here) {
+            word[d] = my_word;
+            logp[d] = my_logp;
         }
     }
 }
@@ -612,7 +647,7 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
     const double *__restrict__ u, uint64_t seed, uint32_t step, int64_t draw0,
     int32_t *__restrict__ word, float *__restrict__ logp)
 {
-    using C = Chunk<T, kDrawThreads, 16>;
+    using C = Chunk<T, kDrawThreads, kDrawPer>;
     constexpr int kLanes = kBlockWords / C::N;  // lanes whose vectors make a block
     __shared__ typename C::Listed listed;
     __shared__ float wave_top[kDrawThreads / 64];
@@ -667,31 +702,35 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
     }
     if (chunks > 1) return;
     __syncthreads();
-    draw_words(x + row * ld, V, r, scale, 1, &own, sum_of, powers, wave, kDrawThreads / 64, draws,
-               row * draws, u, seed, step, draw0, word, logp);
+    constexpr int kWaves = kDrawThreads / 64;
+    const int32_t each = (draws + kWaves - 1) / kWaves, t0 = wave * each;
+    if (t0 < draws)
+        draw_words(x + row * ld, V, r, scale, 1, &own, sum_of, powers, row * draws + t0,
+                   draws - t0 < each ? draws - t0 : each, u, seed, step, draw0, word, logp);
 }
 
-// `share` workgroups of four wavefronts per row.
+// `share` workgroups of four wavefronts per row, `each` draws a wavefront.
 template <typename T>
 __global__ void __launch_bounds__(256) k_draw(const T *__restrict__ x, int64_t ld, int64_t V,
                                               int32_t chunks, spdp_rules rules, double scale,
                                               const Part *__restrict__ part,
                                               const double *__restrict__ blocks, int32_t share,
-                                              int32_t draws, const double *__restrict__ u,
-                                              uint64_t seed, uint32_t step, int64_t draw0,
+                                              int32_t each, int32_t draws,
+                                              const double *__restrict__ u, uint64_t seed,
+                                              uint32_t step, int64_t draw0,
                                               int32_t *__restrict__ word,
                                               float *__restrict__ logp)
 {
-    const int64_t row = blockIdx.x / (uint32_t)share;
-    const int32_t t0 = (int32_t)(blockIdx.x % (uint32_t)share) * 4 + (threadIdx.x >> 6);
     __shared__ Powers powers;
     make_powers(powers);
     __syncthreads();
+    const int64_t row = blockIdx.x / (uint32_t)share;
+    const int64_t t0 = ((int64_t)(blockIdx.x % (uint32_t)share) * 4 + (threadIdx.x >> 6)) * each;
     if (t0 >= draws) return;
     const RowRules r = row_rules(rules, row);
     draw_words(x + row * ld, V, r, scale, chunks, part + row * chunks,
-               blocks + row * chunks * kBlocks, powers, t0, 4 * share, draws, row * draws, u, seed,
-               step, draw0, word, logp);
+               blocks + row * chunks * kBlocks, powers, row * draws + t0,
+               (int32_t)(draws - t0 < each ? draws - t0 : each), u, seed, step, draw0, word, logp);
 }
 
 // launch(value of the scores' type, grid), and its error
@@ -729,6 +768,8 @@ TopShape top_shape(int64_t rows, int64_t V)
 }
 
 int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int64_t kDrawWaves = 16384;
 
 int64_t draw_parts_bytes(int64_t rows, int64_t chunks)
 {
@@ -799,15 +840,16 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
                            word, logp);
     });
     if (e != hipSuccess || chunks == 1) return e;
-    // a wavefront per draw while that leaves the chip's wavefronts enough, then several each
-    int64_t share = (draws + 3) / 4;
-    const int64_t most = (4096 + rows - 1) / rows;
-    share = share > most ? most : share;
+    // a wavefront per draw while that does not fill the chip, then several each
+    int64_t waves = (kDrawWaves + rows - 1) / rows;
+    waves = waves > draws ? draws : waves;
+    const int64_t each = (draws + waves - 1) / waves;
+    const int64_t share = (draws + 4 * each - 1) / (4 * each);
     return by_type(type, rows * share, [&](auto t, dim3 grid) {
         using T = decltype(t);
         hipLaunchKernelGGL(k_draw<T>, grid, dim3(256), 0, st, (const T *)x, ld, V, (int32_t)chunks,
-                           rules, scale, part, blocks, (int32_t)share, draws, u, seed, step, draw0,
-                           word, logp);
+                           rules, scale, part, blocks, (int32_t)share, (int32_t)each, draws, u,
+                           seed, step, draw0, word, logp);
     });
 }
 
