@@ -21,51 +21,90 @@ namespace spdp {
 namespace {
 
 constexpr int kBlock = kBlock8;  // columns that share a scale
-constexpr float kMax8 = 448.0f;  // largest e4m3 value
 
-// Exponent of a block's scale: the least e in [-127, 127] with amax <= 448 2^e.
-// amax = f 2^p with f in [1/2, 1), and 448 = 7/8 2^9.
-__device__ __forceinline__ int scale_exponent(double amax)
+typedef unsigned long long u64;
+
+// Exponent that |x| alone would ask of its block's scale, before it is cut to [-127, 127]:
+// the least e with |x| <= 448 2^e.  |x| = f 2^p with f in [1/2, 1), and 448 = 7/8 2^9, so
+// e = p - 9, and one more where f > 7/8: where adding all but the last of the
+// fraction's upper quarter carries into the exponent.  What is not finite asks for none.
+__device__ __forceinline__ int scale_exponent(double x)
 {
-    if (!(amax > 0.0)) return -127;
-    int p;
-    const double f = frexp(amax, &p);
-    const int e = p - 9 + (f > 0.875 ? 1 : 0);
-    return e < -127 ? -127 : e > 127 ? 127 : e;
+    const u64 bits = __builtin_bit_cast(u64, x) & ~(1ull << 63);
+    const int e = (int)((bits + 0x3FFFFFFFFFFFFull) >> 52) - 1031;
+    return bits < 0x7FF0000000000000ull ? e : -2000;
 }
 
-// v (already scaled) for the 8-bit conversion, which rounds fp32 to nearest even:
-// the value is cut to fp32 with the last bit set where anything was cut off
-// (rounding to odd), so that the two steps round as one.
-__device__ __forceinline__ float odd_f32(double v)
+// x 2^-e as fp32 for the 8-bit conversion, which rounds fp32 to nearest even: cut to fp32
+// with the last bit set where anything was cut off (rounding to odd), so that the two
+// steps round as one.  What the conversion takes to 0 may be 0 here; what is not finite or
+// beyond 448 becomes NaN.
+__device__ __forceinline__ float scaled_odd(double x, int e)
 {
-    if (!(fabs(v) <= (double)kMax8)) return __builtin_nanf("");
-    const float f = __double2float_rz(v);
-    return (double)f == v ? f : __uint_as_float(__float_as_uint(f) | 1u);
+    const u64 bits = __builtin_bit_cast(u64, x);
+    const uint32_t high = (uint32_t)(bits >> 32), low = (uint32_t)bits;
+    const int exponent = (int)(high >> 20 & 0x7FF) - e;  // of the scaled value, 1023 for 1
+    uint32_t f = (uint32_t)((bits & 0xFFFFFFFFFFFFFull) >> 29) | ((low & 0x1FFFFFFF) ? 1u : 0u);
+    f |= (uint32_t)(exponent - 896) << 23;
+    f = exponent < 1000 ? 0u : f;  // (below 2^-23)
+    const bool number = (high & 0x7FF00000u) != 0x7FF00000u && f <= 0x43E00000u;
+    f = number ? f : 0x7FC00000u;
+    return __uint_as_float(f | (high & 0x80000000u));
 }
 
-// One wavefront per (row, block): two columns a lane, the largest finite magnitude
-// over the wavefront, then both values in one 16-bit store.
-template <typename T>
-__global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, int64_t rows, int32_t cols,
-                                               int64_t ld, int32_t nb, uint8_t *__restrict__ q,
-                                               uint8_t *__restrict__ e)
+// The largest of 32 lanes' values, in each of them.
+__device__ __forceinline__ int max32(int v)
 {
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= rows * nb) return;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = unit / nb;
-    const int32_t c = (int32_t)(unit - row * nb) * kBlock + 2 * lane;
-    const T *src = x + row * ld + c;
-    const double a = c < cols ? (double)src[0] : 0.0;
-    const double b = c + 1 < cols ? (double)src[1] : 0.0;
-    double m = fmax(isfinite(a) ? fabs(a) : 0.0, isfinite(b) ? fabs(b) : 0.0);
-    for (int d = 32; d; d >>= 1) m = fmax(m, __shfl_xor(m, d));
-    const int ex = scale_exponent(m);
-    const float fa = odd_f32(ldexp(a, -ex)), fb = odd_f32(ldexp(b, -ex));
-    const int pair = __builtin_amdgcn_cvt_pk_fp8_f32(fa, fb, 0, false);
-    *reinterpret_cast<uint16_t *>(q + unit * kBlock + 2 * lane) = (uint16_t)pair;
-    if (lane == 0) e[unit] = (uint8_t)(ex + 127);
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0xB1, 0xF, 0xF, false));   // lane ^ 1
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x4E, 0xF, 0xF, false));   // lane ^ 2
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x141, 0xF, 0xF, false));  // other 4 of 8
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x140, 0xF, 0xF, false));  // other 8 of 16
+    return max(v, __shfl_xor(v, 16));
+}
+
+// Half a wavefront per (row, block), four columns a lane, UNITS blocks whose columns are all
+// requested first (one of doubles, two of floats: 100 000 rows of 500 take 79 and 58 us); whole numbers throughout, as the scale is an
+// exponent and the rounding bits.
+template <typename T, int UNITS>
+__global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, int64_t units,
+                                               int32_t cols, int64_t ld, int32_t nb,
+                                               uint8_t *__restrict__ q, uint8_t *__restrict__ e)
+{
+    typedef T quad __attribute__((ext_vector_type(4), aligned(4)));
+    const int64_t first = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * UNITS;
+    const int lane = threadIdx.x & 31;
+    double v[UNITS][4];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        const int64_t unit = first + i < units ? first + i : units - 1;
+        const int64_t row = units <= UINT32_MAX ? (uint32_t)unit / (uint32_t)nb : unit / nb;
+        const int32_t c = (int32_t)(unit - row * nb) * kBlock + 4 * lane;
+        const T *src = x + row * ld + c;
+        if (c + 4 <= cols) {
+            const quad a = *reinterpret_cast<const quad *>(src);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i][k] = a[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i][k] = c + k < cols ? (double)src[k] : 0.0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        int ex = -127;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ex = max(ex, scale_exponent(v[i][k]));
+        ex = min(max32(ex), 127);
+        int word = 0;
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_odd(v[i][0], ex), scaled_odd(v[i][1], ex),
+                                               word, false);
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_odd(v[i][2], ex), scaled_odd(v[i][3], ex),
+                                               word, true);
+        if (first + i < units) {
+            *reinterpret_cast<int *>(q + (first + i) * kBlock + 4 * lane) = word;
+            if (lane == 0) e[first + i] = (uint8_t)(ex + 127);
+        }
+    }
 }
 
 typedef __bf16 b2v __attribute__((ext_vector_type(2)));
@@ -501,13 +540,14 @@ hipError_t launch_pack8(const void *x, int32_t type, int64_t rows, int32_t cols,
 {
     const int32_t nb = blocks8(cols);
     if (rows == 0 || nb == 0) return hipSuccess;
-    const dim3 grid((unsigned)((rows * nb + 3) / 4));
+    const int64_t units = rows * nb;
+    const auto blocks = [&](int per) { return dim3((unsigned)((units + 8 * per - 1) / (8 * per))); };
     if (type == SPDP_F64)
-        hipLaunchKernelGGL(k_pack8<double>, grid, dim3(256), 0, st, (const double *)x, rows, cols,
-                           ld, nb, q, e);
+        hipLaunchKernelGGL((k_pack8<double, 1>), blocks(1), dim3(256), 0, st, (const double *)x,
+                           units, cols, ld, nb, q, e);
     else
-        hipLaunchKernelGGL(k_pack8<float>, grid, dim3(256), 0, st, (const float *)x, rows, cols,
-                           ld, nb, q, e);
+        hipLaunchKernelGGL((k_pack8<float, 2>), blocks(2), dim3(256), 0, st, (const float *)x,
+                           units, cols, ld, nb, q, e);
     return hipGetLastError();
 }
 
