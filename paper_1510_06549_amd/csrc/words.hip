@@ -69,6 +69,43 @@ struct Kept {  // LDS
     int in_wave[2][3][kTopWaves];
 };
 
+// The value of another lane: lane ^ 1, lane ^ 2, a lane of the other half of eight, of the
+// other half of sixteen (D = 1, 2, 4, 8).
+template <int D>
+__device__ __forceinline__ int other(int v)
+{
+    constexpr int ctrl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x140;
+    return __builtin_amdgcn_update_dpp(v, v, ctrl, 0xF, 0xF, false);
+}
+
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = fmaxf(v, __int_as_float(other<1>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(other<2>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(other<4>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(other<8>(__float_as_int(v))));
+    float m = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 0));
+    for (int row = 16; row < 64; row += 16)
+        m = fmaxf(m, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), row)));
+    return m;
+}
+
+__device__ __forceinline__ uint32_t wave_or(uint32_t v)
+{
+    v |= (uint32_t)other<1>((int)v);
+    v |= (uint32_t)other<2>((int)v);
+    v |= (uint32_t)other<4>((int)v);
+    v |= (uint32_t)other<8>((int)v);
+    uint32_t m = 0;
+    for (int row = 0; row < 64; row += 16) m |= (uint32_t)__builtin_amdgcn_readlane((int)v, row);
+    return m;
+}
+
+__device__ __forceinline__ u64 wave_or(u64 v)
+{
+    return (u64)wave_or((uint32_t)(v >> 32)) << 32 | wave_or((uint32_t)v);
+}
+
 // Sum over the lanes up to and with each.
 __device__ __forceinline__ int prefix(int v)
 {
@@ -81,9 +118,36 @@ __device__ __forceinline__ int prefix(int v)
     return v;
 }
 
+// Of `group` lanes each (a power of 2, groups in a row) the largest value, and of the groups
+// that are not empty the least of these; for 64 lanes and more, the wavefront's largest.
+__device__ __forceinline__ uint32_t least_largest(uint32_t v, int group, bool empty)
+{
+    const auto step = [&](int d, uint32_t o) { v = d < group ? max(v, o) : min(v, o); };
+    if (group == 1) v = empty ? ~0u : v;
+    step(1, other<1>(v));
+    if (group == 2) v = empty ? ~0u : v;
+    step(2, other<2>(v));
+    if (group == 4) v = empty ? ~0u : v;
+    step(4, other<4>(v));
+    if (group == 8) v = empty ? ~0u : v;
+    step(8, other<8>(v));
+    if (group == 16) v = empty ? ~0u : v;
+    uint32_t row[4];
+    for (int i = 0; i < 4; ++i) row[i] = __builtin_amdgcn_readlane((int)v, 16 * i);
+    uint32_t a = group > 16 ? max(row[0], row[1]) : min(row[0], row[1]);
+    uint32_t b = group > 16 ? max(row[2], row[3]) : min(row[2], row[3]);
+    const u64 none = __ballot(empty);
+    if (group == 32) {
+        a = none & 1 ? ~0u : a;
+        b = none >> 32 & 1 ? ~0u : b;
+    }
+    a = group > 32 ? max(a, b) : min(a, b);
+    return group == 64 && (none & 1) ? ~0u : a;
+}
+
 // Places for `mine` keys of each thread, in the threads' order: the thread's first place
-// behind `before`, and in total how many places there are.  All threads call it; `slot` may
-// be used again behind the next barrier but one.
+// behind `before`, and in total how many places there are.  All threads call it, and meet
+// a barrier; `slot` may be used again behind the next one.
 __device__ __forceinline__ int places(int mine, int before, int (&slot)[kTopWaves], int &total)
 {
     const int upto = prefix(mine), wave = threadIdx.x >> 6;
@@ -117,10 +181,8 @@ __device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
             all &= key[i];
         }
     }
-    for (int d = 32; d; d >>= 1) {
-        any |= __shfl_xor(any, d);
-        all &= __shfl_xor(all, d);
-    }
+    any = wave_or(any);
+    all = ~wave_or(~all);
     __syncthreads();
     if (lane == 0) {
         kept.key[2 * wave] = any;
@@ -170,14 +232,23 @@ __device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
 }
 
 // Calls put(rank, key) for the k largest of the n keys, n <= kTopThreads: a key's rank is
-// the number of larger ones.
+// the number of larger ones.  All threads call it, behind a barrier.
 template <typename F>
-__device__ __forceinline__ void rank_keys(const Kept &kept, int n, int k, F put)
+__device__ __forceinline__ void rank_keys(Kept &kept, int n, int k, F put)
 {
+    constexpr int kAtOnce = 8;  // keys read at a time
+    if ((int)threadIdx.x < kAtOnce) kept.key[n + threadIdx.x] = 0;
+    __syncthreads();
     if ((int)threadIdx.x >= n) return;
     const u64 key = kept.key[threadIdx.x];
     int rank = 0;
-    for (int i = 0; i < n; ++i) rank += kept.key[i] > key;
+    for (int i = 0; i < n; i += kAtOnce) {
+        u64 o[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) o[j] = kept.key[i + j];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) rank += o[j] > key;
+    }
     if (rank < k) put(rank, key);
 }
 
@@ -206,8 +277,8 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     using C = Chunk<T, kTopThreads, 16>;
     __shared__ typename C::Listed listed;
     __shared__ Kept kept;
-    __shared__ uint32_t wave_least[kTopWaves];
-    __shared__ int wave_pass[kTopWaves];
+    __shared__ uint32_t wave_least[2][kTopWaves];
+    __shared__ int wave_pass[2][kTopWaves];
     const int64_t row = blockIdx.x / (uint32_t)parts;
     const int64_t first = (int64_t)(blockIdx.x % (uint32_t)parts) * words;
     const int64_t end = first + words < V ? first + words : V;
@@ -221,11 +292,20 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     const int threads = holding < kTopThreads ? (int)holding : kTopThreads;
     int group = 1;
     while (group < kTopThreads && (threads + 2 * group - 1) / (2 * group) >= k) group *= 2;
-    const bool grouped = threads >= k, holds = (int)threadIdx.x < threads;
+    const bool grouped = threads >= k, empty = (int)(threadIdx.x / group * group) >= threads;
+    const int wave = threadIdx.x >> 6;
     int n = 0;           // keys kept
     uint32_t mine = 0;   // largest order that this thread has seen
     u64 bound = 1;       // keys below are not among the k best
-    for (int64_t w0 = first; w0 < end; w0 += C::kWords) {
+    auto raise = [&](const uint32_t (&w)[kTopWaves]) {
+        const uint32_t least = group <= 64    ? min(min(w[0], w[1]), min(w[2], w[3]))
+                               : group == 128 ? min(max(w[0], w[1]), max(w[2], w[3]))
+                                              : max(max(w[0], w[1]), max(w[2], w[3]));
+        const u64 b = (u64)least << 32;
+        bound = grouped && b > bound ? b : bound;
+    };
+    int turn = 0;
+    for (int64_t w0 = first; w0 < end; w0 += C::kWords, turn ^= 1) {
         if (r.n_words > 0) C::count(r, w0, listed);
         uint32_t order[C::U][C::N];
 #pragma unroll
@@ -239,27 +319,11 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
             }
         }
         if (w0 + C::kWords < end) c.request(x, w0 + C::kWords, end);
-        // least of the groups' largest
-        uint32_t g = holds ? mine : 0;
-        for (int d = 1; d < group && d < 64; d *= 2) {
-            const uint32_t o = __shfl_xor(g, d);
-            g = o > g ? o : g;
-        }
-        // (a group without words does not count)
-        if ((int)(threadIdx.x / group * group) >= threads) g = ~0u;
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t o = __shfl_xor(g, d);
-            g = o < g ? o : g;
-        }
-        if ((threadIdx.x & 63) == 0) wave_least[threadIdx.x >> 6] = g;
-        __syncthreads();
-        if (grouped) {
-            const uint32_t *w = wave_least;
-            const uint32_t least = group <= 64    ? min(min(w[0], w[1]), min(w[2], w[3]))
-                                   : group == 128 ? min(max(w[0], w[1]), max(w[2], w[3]))
-                                                  : max(max(w[0], w[1]), max(w[2], w[3]));
-            const u64 b = (u64)least << 32;
-            bound = b > bound ? b : bound;
+        const uint32_t least = least_largest(mine, group, empty);
+        if ((threadIdx.x & 63) == 0) wave_least[turn][wave] = least;
+        if (w0 == first) {  // (later chunks go by the bound of the ones before)
+            __syncthreads();
+            raise(wave_least[turn]);
         }
         const uint32_t low = (uint32_t)(bound >> 32) > 1 ? (uint32_t)(bound >> 32) : 1;
         uint32_t pass = 0;
@@ -268,7 +332,8 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
 #pragma unroll
             for (int i = 0; i < C::N; ++i)
                 pass |= (uint32_t)(order[u][i] >= low) << (u * C::N + i);
-        int passing, to = places(__builtin_popcount(pass), n, wave_pass, passing);
+        int passing, to = places(__builtin_popcount(pass), n, wave_pass[turn], passing);
+        raise(wave_least[turn]);
         if (n + passing <= kKeys) {
             if (pass) {
 #pragma unroll
@@ -279,7 +344,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
                             kept.key[to++] = key_of(order[u][i], w0 + C::at(u) + i);
             }
             n += passing;
-            __syncthreads();
+            if (r.n_words > 0) __syncthreads();  // (before the next chunk's words are counted)
             continue;
         }
         // (kKeys / 2 scores at a time, so that there is room after every cut)
@@ -300,7 +365,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
                     key[e] = key_of(order[u][i + e], w0 + C::at(u) + i + e);
                     more += key[e] >= bound;
                 }
-                int at = places(more, n, wave_pass, passing);
+                int at = places(more, n, wave_pass[0], passing);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (key[e] >= bound) kept.key[at++] = key[e];
@@ -308,6 +373,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
             }
         __syncthreads();
     }
+    __syncthreads();
     if (n > kTopThreads) {
         u64 least;
         n = cut_keys(kept, n, k, least);
@@ -516,7 +582,7 @@ __device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double s
         is = is && t == t;
         top = fmaxf(top, t);
     }
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    top = wave_max(top);
     law.top = top;
     law.is = !__any(!is) && top > -__builtin_inff();
     if (law.is)
@@ -675,7 +741,7 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
             top = fmaxf(top, v[k][i]);
         }
     }
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    top = wave_max(top);
     if (lane == 0) wave_top[wave] = top;
     law = !__syncthreads_or(!law);
     for (int i = 0; i < kDrawThreads / 64; ++i) top = fmaxf(top, wave_top[i]);
