@@ -433,14 +433,14 @@ __global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict_
 //
 // One pass over the scores leaves of every chunk its largest score, the sum of its
 // weights relative to that (the largest is then 1 in every chunk, and they do not
-// vanish beside the row's largest), and the sums of its blocks of 128 words.  A draw
-// is then one wavefront's work: the chunk among the chunks' sums, the block among its
-// chunk's 64, the word among its block's 128 scores, each by a prefix sum over the
-// lanes.
+// vanish beside the row's largest), and the sums up to the end of each of its blocks of
+// 64 words.  A draw is then one wavefront's work: the chunk among the chunks, the block
+// among its chunk's 128, the word among its block's 64 scores, by where the target
+// falls between the sums up to one and up to the next.
 // ---------------------------------------------------------------------------
 constexpr int kDrawThreads = 512, kDrawPer = 16;
 constexpr int kDrawChunk = kDrawThreads * kDrawPer;
-constexpr int kBlocks = 64, kBlockWords = kDrawChunk / kBlocks;
+constexpr int kBlockWords = 64, kBlocks = kDrawChunk / kBlockWords;  // two blocks a lane
 
 struct Part {
     double top, sum;  // top: NaN where the chunk holds NaN or +inf
@@ -486,14 +486,21 @@ __device__ __forceinline__ double weight_of(float x, double top, double scale, c
     return power_of(((double)x - top) * scale, p);
 }
 
-// The value that DPP control CTRL brings to a lane, 0 where it brings none.
+// The value that DPP control CTRL brings to a lane; 0 where it brings none, and in the rows
+// of 16 lanes that are not among ROWS.
 template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ double moved(double v)
 {
     const u64 b = __builtin_bit_cast(u64, v);
-    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF,
-                                                    false);
+    const int l = (int)(uint32_t)b, h = (int)(uint32_t)(b >> 32);
+    uint32_t lo, hi;
+    if constexpr (ROWS == 0xF) {
+        lo = __builtin_amdgcn_mov_dpp(l, CTRL, 0xF, 0xF, true);
+        hi = __builtin_amdgcn_mov_dpp(h, CTRL, 0xF, 0xF, true);
+    } else {
+        lo = __builtin_amdgcn_update_dpp(0, l, CTRL, ROWS, 0xF, false);
+        hi = __builtin_amdgcn_update_dpp(0, h, CTRL, ROWS, 0xF, false);
+    }
     return __builtin_bit_cast(double, (u64)hi << 32 | lo);
 }
 
@@ -518,36 +525,64 @@ __device__ __forceinline__ double prefix(double v)
     return v;
 }
 
-// Sum over groups of 16 or 32 lanes, in each of their lanes.
+// Sum over groups of 8 or 16 lanes, in each of their lanes.
 template <int LANES>
 __device__ __forceinline__ double group_sum(double v)
 {
     v += moved<0xB1>(v);   // lane ^ 1
     v += moved<0x4E>(v);   // lane ^ 2
     v += moved<0x141>(v);  // the other four of eight
-    v += moved<0x140>(v);  // the other eight of sixteen
-    if constexpr (LANES == 32) v += __shfl_xor(v, 16);
+    if constexpr (LANES == 16) v += moved<0x140>(v);  // the other eight of sixteen
     return v;
 }
 
-// A choice among 64 shares with the sums `upto`: the first lane whose sum exceeds goal,
-// else (rounding, or goal infinite) the last with a share; goal becomes what is left of
-// it, at least 0.  Some share has to be positive.
-__device__ __forceinline__ int choose(double share, double upto, double &goal)
+// The largest of the lanes up to and with each, of values >= 0.
+__device__ __forceinline__ double largest_upto(double v)
 {
-    const u64 positive = __ballot(share > 0.0);
-    const u64 past = __ballot(upto > goal) & positive;
-    const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(positive);
-    goal = fmax(goal - of_lane(upto - share, at), 0.0);
-    return at;
+    v = fmax(v, moved<0x111>(v));
+    v = fmax(v, moved<0x112>(v));
+    v = fmax(v, moved<0x114>(v));
+    v = fmax(v, moved<0x118>(v));
+    v = fmax(v, moved<0x142, 0xA>(v));
+    return fmax(v, moved<0x143, 0xC>(v));
+}
+
+__device__ __forceinline__ double lane_before(double v)  // (0 for the first)
+{
+    const double o = __shfl_up(v, 1);
+    return (threadIdx.x & 63) ? o : 0.0;
+}
+
+// Two shares a lane, in order: upto[i] the sum up to and with share i.  The sums of different
+// lanes are rounded differently, so they are made to rise: never below the one before,
+// and above it only where there is a share.
+__device__ __forceinline__ void rising(const double (&share)[2], double (&upto)[2])
+{
+    const double all = prefix(share[0] + share[1]);
+    const double a = share[0] > 0.0 ? lane_before(all) + share[0] : 0.0;
+    const double b = share[1] > 0.0 ? all : 0.0;
+    const double before = lane_before(largest_upto(fmax(a, b)));
+    upto[0] = fmax(before, a);
+    upto[1] = fmax(upto[0], b);
+}
+
+// The lane whose sum is the first to exceed goal, else (goal infinite, or rounding) the
+// first that reaches the last sum, which has to be positive: in either case one with a
+// share.
+__device__ __forceinline__ int choose(double upto, double goal)
+{
+    u64 lanes = __ballot(upto > goal);
+    if (!lanes) lanes = __ballot(upto == of_lane(upto, 63));
+    return __builtin_ctzll(lanes);
 }
 
 // What a row's draws share.
 struct Law {
-    double top, total;  // largest score; sum of the weights
-    double share, upto; // this lane's chunk: its share of the weights, the sum up to it,
-    double own, inverse; // its largest score, and by what its own weights exceed their share
-    int32_t last;       // first of the last 64 chunks that hold some weight
+    double top, total;    // largest score; sum of the weights
+    double upto;          // sum of the weights up to and with this lane's chunk;
+    double own, inverse;  // its largest score, and by what its own weights exceed theirs
+    bool some;            // whether it holds some weight
+    int32_t last;         // first of the last 64 chunks that hold some weight
     bool is;
 };
 
@@ -555,19 +590,21 @@ struct Law {
 __device__ __forceinline__ void lane_chunk(Law &law, const Part *part, int32_t c, int32_t chunks,
                                            double scale, const Powers &powers)
 {
-    law.share = 0.0;
+    double share = 0.0;
     law.own = law.top;
     law.inverse = 1.0;
     if (c < chunks) {
         const Part p = part[c];
         if (p.sum > 0.0) {
             const double w = power_of((p.top - law.top) * scale, powers);
-            law.share = p.sum * w;
+            share = p.sum * w;
             law.own = p.top;
             law.inverse = 1.0 / w;
         }
     }
-    law.upto = prefix(law.share);
+    law.some = share > 0.0;
+    const double upto = prefix(share);
+    law.upto = largest_upto(law.some ? upto : 0.0);
 }
 
 __device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double scale,
@@ -589,7 +626,7 @@ __device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double s
         for (int32_t c0 = 0; c0 < chunks; c0 += 64) {
             lane_chunk(law, part, c0 + lane, chunks, scale, powers);
             law.total += of_lane(law.upto, 63);
-            if (__any(law.share > 0.0)) law.last = c0;
+            if (of_lane(law.upto, 63) > 0.0) law.last = c0;
         }
     return law;
 }
@@ -640,54 +677,68 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
                         goal -= sum;
                     }
                 }
-                const int at = choose(law.share, law.upto, goal);
-                const double own = of_lane(law.own, at), inverse = of_lane(law.inverse, at);
-                goal = goal > 0.0 ? goal * inverse : 0.0;
-                const double share = blocks[(int64_t)(c0 + at) * kBlocks + lane];
-                const int b = choose(share, prefix(share), goal);
-                // the block's words, two a lane: everything that is read of them at once
-                const int64_t b0 = (int64_t)(c0 + at) * kDrawChunk + b * kBlockWords;
-                const int64_t w = b0 + 2 * lane;
-                float s[2] = {0.f, 0.f}, bias[2] = {0.f, 0.f};
-                uint32_t allowed = 3;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (w + i < V) {
-                        s[i] = (float)x[w + i];
-                        if (r.bias) bias[i] = r.bias[w + i];
-                    }
-                if (r.mask && w < V) allowed = r.mask[w >> 5] >> (w & 31);
-                int32_t n[2] = {0, 0};
-                auto tally = [&](int32_t entry) {
-                    const uint32_t a = (uint32_t)entry - (uint32_t)b0;
-                    u64 hits = __ballot(a < (uint32_t)kBlockWords && entry >= 0);
-                    while (hits) {
-                        const int h = __builtin_amdgcn_readlane((int)a, __builtin_ctzll(hits));
-                        hits &= hits - 1;
-                        n[0] += h == 2 * lane;
-                        n[1] += h == 2 * lane + 1;
-                    }
-                };
-#pragma unroll
-                for (int i = 0; i < kListed; ++i)
-                    if (i * 64 < r.n_words) tally(listed[i]);
-                for (int64_t i = kListed * 64; i < r.n_words; i += 64)
-                    tally(i + lane < r.n_words ? r.words[i + lane] : -1);
-                double y[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (n[i] > 0) s[i] = penalised(r, s[i], n[i]);
-                    if (r.bias) s[i] = s[i] + bias[i];
-                    s[i] = (allowed >> i & 1u) && w + i < V ? s[i] : -__builtin_inff();
-                    y[i] = weight_of(s[i], own, scale, powers);
+                // (an infinite goal: the last word with weight, however little it adds)
+                const bool end = !(goal < __builtin_inf());
+                const int at = end ? 63 - __builtin_clzll(__ballot(law.some))
+                                   : choose(law.upto, goal);
+                const double own = of_lane(law.own, at);
+                int b = kBlocks - 1;
+                if (!end) {
+                    if (at) goal -= of_lane(law.upto, at - 1);
+                    goal = goal > 0.0 ? goal * of_lane(law.inverse, at) : 0.0;
+                    const double2 upto = reinterpret_cast<const double2 *>(
+                        blocks + (int64_t)(c0 + at) * kBlocks)[lane];
+                    const int pair = choose(upto.y, goal);
+                    const double mid = of_lane(upto.x, pair), last = of_lane(upto.y, pair);
+                    const bool second = last > goal ? !(mid > goal) : mid < last;
+                    const double before = second ? mid : pair ? of_lane(upto.y, pair - 1) : 0.0;
+                    goal = fmax(goal - before, 0.0);
+                    b = 2 * pair + second;
                 }
-                const double both = y[0] + y[1];
-                const int l = choose(both, prefix(both), goal);
-                const bool second = !(y[0] > goal) && y[1] > 0.0;
-                const int32_t got = __builtin_amdgcn_readlane((int)(w + second), l);
-                const float score = __builtin_bit_cast(
-                    float, __builtin_amdgcn_readlane(
-                               __builtin_bit_cast(int, second ? s[1] : s[0]), l));
+                int64_t b0;
+                float s;
+                double weight;
+                u64 positive;
+                for (;; --b) {
+                    // the block's words, one a lane: everything that is read of them at once
+                    b0 = (int64_t)(c0 + at) * kDrawChunk + b * kBlockWords;
+                    const int64_t w = b0 + lane;
+                    float bias = 0.f;
+                    uint32_t allowed = 0;
+                    s = 0.f;
+                    if (w < V) {
+                        s = (float)x[w];
+                        if (r.bias) bias = r.bias[w];
+                        allowed = r.mask ? r.mask[w >> 5] >> (w & 31) : 1;
+                    }
+                    int32_t n = 0;
+                    auto tally = [&](int32_t entry) {
+                        const uint32_t a = (uint32_t)entry - (uint32_t)b0;
+                        u64 hits = __ballot(a < (uint32_t)kBlockWords && entry >= 0);
+                        while (hits) {
+                            n += __builtin_amdgcn_readlane((int)a, __builtin_ctzll(hits)) == lane;
+                            hits &= hits - 1;
+                        }
+                    };
+#pragma unroll
+                    for (int i = 0; i < kListed; ++i)
+                        if (i * 64 < r.n_words) tally(listed[i]);
+                    for (int64_t i = kListed * 64; i < r.n_words; i += 64)
+                        tally(i + lane < r.n_words ? r.words[i + lane] : -1);
+                    if (n > 0) s = penalised(r, s, n);
+                    if (r.bias) s = s + bias;
+                    s = allowed & 1u ? s : -__builtin_inff();
+                    weight = weight_of(s, own, scale, powers);
+                    positive = __ballot(weight > 0.0);
+                    // (a chunk's largest score has weight 1, so the search ends)
+                    if (positive || b == 0) break;
+                }
+                const double sums = prefix(weight);
+                const u64 past = __ballot(sums > goal) & positive;
+                const int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(positive | 1);
+                const int32_t got = (int32_t)(b0 + l);
+                const float score =
+                    __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s), l));
                 if (lane == t) {
                     my_word = got;
                     my_logp = score;
@@ -707,7 +758,7 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
 // One workgroup per (row, chunk): its largest score and its sums.  Rows of one chunk are
 // drawn from at once.
 template <typename T>
-__global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
+__global__ void __launch_bounds__(kDrawThreads, 8) k_draw_parts(
     const T *__restrict__ x, int64_t ld, int64_t V, int32_t chunks, spdp_rules rules, double scale,
     Part *__restrict__ part, double *__restrict__ blocks, int32_t draws,
     const double *__restrict__ u, uint64_t seed, uint32_t step, int64_t draw0,
@@ -717,7 +768,7 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
     constexpr int kLanes = kBlockWords / C::N;  // lanes whose vectors make a block
     __shared__ typename C::Listed listed;
     __shared__ float wave_top[kDrawThreads / 64];
-    __shared__ double sum_of[kBlocks];
+    __shared__ alignas(16) double sum_of[kBlocks];
     __shared__ Part own;
     __shared__ Powers powers;
     make_powers(powers);
@@ -759,11 +810,16 @@ __global__ void __launch_bounds__(kDrawThreads) k_draw_parts(
     }
     __syncthreads();
     if (wave == 0) {
-        const double s = sum_of[lane], sum = of_lane(prefix(s), 63);
-        if (lane == 0) own = Part{law ? (double)top : __builtin_nan(""), sum};
-        if (chunks > 1) {
-            blocks[(int64_t)blockIdx.x * kBlocks + lane] = s;
-            if (lane == 0) part[blockIdx.x] = Part{law ? (double)top : __builtin_nan(""), sum};
+        const double share[2] = {sum_of[2 * lane], sum_of[2 * lane + 1]};
+        double upto[2];
+        rising(share, upto);
+        const Part p{law ? (double)top : __builtin_nan(""), of_lane(upto[1], 63)};
+        double *to = chunks > 1 ? blocks + (int64_t)blockIdx.x * kBlocks : sum_of;
+        to[2 * lane] = upto[0];
+        to[2 * lane + 1] = upto[1];
+        if (lane == 0) {
+            own = p;
+            if (chunks > 1) part[blockIdx.x] = p;
         }
     }
     if (chunks > 1) return;
