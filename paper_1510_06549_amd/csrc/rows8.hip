@@ -463,13 +463,11 @@ Shares shares_of(int64_t m, int64_t n, int32_t fd)
     return s;
 }
 
-// Scores above this many bytes are written past the caches' order.  Below, they stay in
-// the last level cache for whoever reads them next, and take less time too (777 x
-// 14 724 in fp16, 23 MB: 11.2 us, 15.0 streamed); above, they would push out the words,
-// which every tile of documents reads again (2 000 x 100 000 in bf16, 400 MB: 237 us, 192
-// streamed; 1 000 x 100 000 of 64 topics in fp16, 200 MB: 72 and 56 us).
-constexpr int64_t kStreamBytes = 64 << 20;
-
+// Scores above kStreamBytes are written past the caches' usual order: they would push out
+// the words, which every tile of documents reads again (2 000 x 100 000 in bf16, 400 MB: 237
+// us, 192 streamed; 1 000 x 100 000 of 64 topics in fp16, 200 MB: 72 and 56 us).  Less than
+// that stays in the last level cache for whoever reads it next, and takes less time too (777
+// x 14 724 in fp16, 23 MB: 11.2 us, 15.0 streamed).
 template <typename T, bool LOG, int FD, bool STREAM>
 hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
 {

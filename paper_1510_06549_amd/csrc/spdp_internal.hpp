@@ -355,6 +355,7 @@ double align_topics_host(const double *c, int32_t kp, int32_t kq, int32_t *match
 // Words of documents (rows8.hip, words.hip).  Sizes and buffers are checked at the
 // boundary; rules hold null pointers for parts that are left out.
 constexpr int32_t kBlock8 = SPDP_BLOCK8;
+constexpr int64_t kStreamBytes = 64 << 20;    // scores above it are streamed past the caches
 constexpr int64_t kPredictScores = 96 << 20;  // bytes of scores that spdp_predict holds at a time
 inline int32_t blocks8(int32_t cols) { return (cols + kBlock8 - 1) / kBlock8; }
 hipError_t launch_pack8(const void *x, int32_t type, int64_t rows, int32_t cols, int64_t ld,

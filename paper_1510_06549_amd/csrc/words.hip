@@ -10,12 +10,12 @@ typedef unsigned long long u64;
 // One workgroup per (row, chunk).
 constexpr int kAdjustThreads = 512;
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(kAdjustThreads) k_adjust(const T *x, int64_t ldx, T *y,
                                                            int64_t ldy, int64_t V, int32_t chunks,
                                                            spdp_rules rules)
 {
-    using C = Chunk<T, kAdjustThreads, 16>;
+    using C = Chunk<T, kAdjustThreads, 16, STREAM>;
     __shared__ typename C::Listed listed;
     const int64_t row = blockIdx.x / (uint32_t)chunks;
     const int64_t w0 = (int64_t)(blockIdx.x % (uint32_t)chunks) * C::kWords;
@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kAdjustThreads) k_adjust(const T *x, int64_t l
         for (int i = 0; i < C::N; ++i) k.v[i] = (T)v[i];
         const int a = C::at(u);
         if (w0 + a + C::N <= V) {
-            store_vec(out + a, k);
+            store_vec<STREAM>(out + a, k);
         } else {
 #pragma unroll
             for (int i = 0; i < C::N; ++i)
@@ -900,6 +900,7 @@ int64_t draw_parts_bytes(int64_t rows, int64_t chunks)
 
 }  // namespace
 
+// (1 000 x 100 000 in bf16 with all rules, 200 MB in and out: 93 us streamed, 98 not)
 hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
                          int64_t rows, int64_t V, const spdp_rules &rules, hipStream_t st)
 {
@@ -907,8 +908,10 @@ hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32
     const int64_t chunks = chunks_of(V, kAdjustThreads * 16);
     return by_type(type, rows * chunks, [&](auto t, dim3 grid) {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_adjust<T>, grid, dim3(kAdjustThreads), 0, st, (const T *)x, ldx,
-                           (T *)y, ldy, V, (int32_t)chunks, rules);
+        const auto kernel = rows * V * (int64_t)sizeof(T) > kStreamBytes ? k_adjust<T, true>
+                                                                         : k_adjust<T, false>;
+        hipLaunchKernelGGL(kernel, grid, dim3(kAdjustThreads), 0, st, (const T *)x, ldx, (T *)y,
+                           ldy, V, (int32_t)chunks, rules);
     });
 }
 

@@ -29,23 +29,28 @@ struct Vec {
     T v[N];
 };
 
-template <typename T>
+// STREAM: past the caches' usual order, for scores that are more than the caches hold.
+template <bool STREAM, typename T>
 __device__ __forceinline__ Vec<T> load_vec(const T *p)
 {
     typedef int unit __attribute__((ext_vector_type(4), aligned(2)));
-    const auto u = *reinterpret_cast<const unit *>(p);
+    const unit *q = reinterpret_cast<const unit *>(p);
+    unit u;
+    if constexpr (STREAM) u = __builtin_nontemporal_load(q);
+    else u = *q;
     Vec<T> k;
     __builtin_memcpy(&k, &u, sizeof k);
     return k;
 }
 
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void store_vec(T *p, const Vec<T> &k)
 {
     typedef int unit __attribute__((ext_vector_type(4), aligned(2)));
     unit u;
     __builtin_memcpy(&u, &k, sizeof k);
-    *reinterpret_cast<unit *>(p) = u;
+    if constexpr (STREAM) __builtin_nontemporal_store(u, reinterpret_cast<unit *>(p));
+    else *reinterpret_cast<unit *>(p) = u;
 }
 
 // The rules of one row.
@@ -108,10 +113,10 @@ __device__ __forceinline__ float ruled(const RowRules &r, float x, int64_t w, in
 
 // The chunk of a row that a workgroup of THREADS threads holds, PER scores a thread in
 // vectors of 16 bytes: vector u of a thread is at (u THREADS + thread) N of the chunk.
-template <typename T, int THREADS, int PER>
+template <typename T, int THREADS, int PER, bool STREAM = false>
 struct Chunk {
     static constexpr int kWords = THREADS * PER, N = Vec<T>::N, U = PER / N;
-    struct Listed {  // LDS
+    struct alignas(16) Listed {  // LDS
         uint32_t seen[kWords / 32];
         int32_t count[kWords];
     };
@@ -126,7 +131,7 @@ struct Chunk {
         for (int u = 0; u < U; ++u) {
             const int64_t w = w0 + at(u);
             if (w + N <= V) {
-                raw[u] = load_vec(row + w);
+                raw[u] = load_vec<STREAM>(row + w);
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i) raw[u].v[i] = w + i < V ? row[w + i] : (T)0;
@@ -139,18 +144,24 @@ struct Chunk {
     // a barrier has to come before it is called again.
     static __device__ __forceinline__ void count(const RowRules &r, int64_t w0, Listed &l)
     {
-        for (int i = threadIdx.x; i < kWords / 32; i += THREADS) l.seen[i] = 0;
-        for (int64_t i = threadIdx.x; i < r.n_words; i += THREADS) {
-            const int64_t a = (int64_t)r.words[i] - w0;
-            if (a >= 0 && a < kWords) l.count[a] = 0;
-        }
+        // (a thread's first word is on its way while the counts are cleared)
+        int32_t word = (int64_t)threadIdx.x < r.n_words ? r.words[threadIdx.x] : -1;
+        typedef int quad __attribute__((ext_vector_type(4)));
+        quad *clear = reinterpret_cast<quad *>(&l);
+        constexpr int kQuads = (int)(sizeof(Listed) / sizeof(quad));
+#pragma unroll
+        for (int i = 0; i < (kQuads + THREADS - 1) / THREADS; ++i)
+            if (i * THREADS + (int)threadIdx.x < kQuads) clear[i * THREADS + threadIdx.x] = quad{0, 0, 0, 0};
         __syncthreads();
-        for (int64_t i = threadIdx.x; i < r.n_words; i += THREADS) {
-            const int64_t a = (int64_t)r.words[i] - w0;
-            if (a >= 0 && a < kWords) {
+        for (int64_t i = threadIdx.x;;) {
+            const int64_t a = (int64_t)word - w0;
+            if (word >= 0 && a >= 0 && a < kWords) {
                 atomicAdd(&l.count[a], 1);
                 atomicOr(&l.seen[a >> 5], 1u << (a & 31));
             }
+            i += THREADS;
+            if (i >= r.n_words) break;
+            word = r.words[i];
         }
         __syncthreads();
     }
