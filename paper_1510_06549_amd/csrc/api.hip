@@ -1328,7 +1328,7 @@ int spdp_predict_work(int64_t docs, int32_t n_words, int32_t type, int32_t k, in
     if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
         return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
     int64_t rows = kPredictScores / (n_words * type_size(type));
-    rows = rows < 1 ? 1 : rows;
+    rows = rows < 1 ? 1 : rows > kPredictTile ? rows - rows % kPredictTile : rows;
     rows = rows < docs ? rows : docs;
     *bytes = scores_room(rows, n_words, type, false) + words_work(rows, n_words, k);
     return SPDP_OK;
@@ -1359,8 +1359,16 @@ int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
         return scores_room(rows, V, a.type, kept) + (choose ? words_work(rows, V, a.k) : 0);
     };
     if (!kept && !choose) return SPDP_OK;  // nothing asked for
-    int64_t rows = D;  // documents at a time
-    while (rows > 1 && need(rows) > work_bytes) rows = (rows + 1) / 2;
+    // documents at a time: as many as there is room for, in whole tiles of the product
+    int64_t rows = D;
+    if (need(D) > work_bytes) {
+        int64_t low = 1;
+        while (rows - low > 1) {
+            const int64_t mid = low + (rows - low) / 2;
+            (need(mid) <= work_bytes ? low : rows) = mid;
+        }
+        rows = low > kPredictTile ? low - low % kPredictTile : low;
+    }
     CALL(check_work(work, work_bytes, need(rows)));
     CALL(check_blocks(words_blocks(rows, V)));
     CALL(check_blocks((rows + 15) / 16 * ((V + 15) / 16)));
