@@ -312,10 +312,10 @@ int spdp_align_topics(const double *h, int32_t kp, int32_t kq, int32_t *match, d
  * runs them in one call.  They use the state's device and stream only (the
  * state's counts are neither read nor changed), take device pointers only, allocate
  * nothing and do not synchronise: they can be captured into a HIP graph.
- * Buffers are checked to be device memory that holds their size (against the
- * device allocation, not against a caller's sub-range of it); what they hold
- * is not checked on the host, and each entry point says what becomes of values
- * out of range.  A workspace belongs to one call at a time: calls that overlap
+ * Buffers are checked to be memory of the state's device that holds their size
+ * (against the device allocation, not against a caller's sub-range of it), aligned to
+ * their elements; what they hold is not checked on the host, and each entry point says
+ * what becomes of values out of range.  A workspace belongs to one call at a time: calls that overlap
  * (other streams, other graphs) need workspaces of their own.
  */
 
@@ -402,8 +402,8 @@ typedef struct {
 /*
  * y = x' : scores x under the rules (device [rows][n_words], ldx and ldy elements
  * from one row to the next, both of `type` SPDP_F32, SPDP_F16 or SPDP_BF16).  y may be x with
- * ldy = ldx; other overlaps are an error.  Elements behind a row's end are left as
- * they are.
+ * ldy = ldx; other overlaps, of the memory from the first element to the last, are an
+ * error.  Elements behind a row's end are left as they are.
  * Errors: E_ARG (NULL pointer, sizes out of range, rules of another size or
  * incomplete, another type, overlapping buffers, buffers as for spdp_pack8),
  * E_RANGE (more than 2^31 chunks of 4096 scores), E_HIP.

@@ -1060,11 +1060,13 @@ private:
     hipError_t err_;
 };
 
-// That [p, p + bytes) lies in one device allocation.
-int check_device(const void *p, int64_t bytes, const char *name)
+// That [p, p + bytes) lies in one allocation of the state's device, at a multiple of `unit`
+// bytes.
+int check_device(const spdp_state *s, const void *p, int64_t bytes, int unit, const char *name)
 {
     if (bytes == 0) return SPDP_OK;
     if (!p) return fail(SPDP_E_ARG, "%s is NULL", name);
+    if ((uintptr_t)p % unit != 0) return fail(SPDP_E_ARG, "%s is misaligned", name);
     hipDeviceptr_t base = nullptr;
     size_t size = 0;
     if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess) {
@@ -1074,6 +1076,17 @@ int check_device(const void *p, int64_t bytes, const char *name)
     const int64_t at = static_cast<const char *>(p) - static_cast<const char *>(base);
     if (bytes > (int64_t)size - at)
         return fail(SPDP_E_ARG, "%s: %lld bytes run past its allocation", name, (long long)bytes);
+    static const int devices = [] {
+        int n = 0;
+        return hipGetDeviceCount(&n) == hipSuccess ? n : 0;
+    }();
+    if (devices > 1) {
+        hipPointerAttribute_t a{};
+        if (hipPointerGetAttributes(&a, p) != hipSuccess || a.device != s->device) {
+            (void)hipGetLastError();
+            return fail(SPDP_E_ARG, "%s is not memory of the state's device", name);
+        }
+    }
     return SPDP_OK;
 }
 
@@ -1100,8 +1113,8 @@ int matrix_bytes(int64_t rows, int64_t n, int64_t ld, int32_t type, const char *
 }
 
 // Rows of scores: their type, sizes and buffer.
-int check_scores(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t n,
-                 const char *name)
+int check_scores(const spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
+                 int64_t n, const char *name)
 {
     if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
         return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
@@ -1109,22 +1122,21 @@ int check_scores(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t 
         return fail(SPDP_E_ARG, "need 0 <= rows < 2^31 and 1 <= n_words < 2^31");
     int64_t bytes = 0;
     CALL(matrix_bytes(rows, n, ld, type, name, &bytes));
-    if ((uintptr_t)x % type_size(type) != 0) return fail(SPDP_E_ARG, "%s is misaligned", name);
-    return check_device(x, bytes, name);
+    return check_device(s, x, bytes, (int)type_size(type), name);
 }
 
-int check_rows8(const spdp_rows8 *a, const char *name)
+int check_rows8(const spdp_state *s, const spdp_rows8 *a, const char *name)
 {
     if (!a) return fail(SPDP_E_ARG, "%s is NULL", name);
     if (a->rows < 0 || a->rows > INT32_MAX || a->cols < 1 || a->cols >= 1 << 24)
         return fail(SPDP_E_ARG, "%s: need 0 <= rows < 2^31 and 1 <= cols < 2^24", name);
     if (!aligned16(a->q)) return fail(SPDP_E_ARG, "%s: q is not 16-byte aligned", name);
     const int64_t blocks = a->rows * blocks8(a->cols);
-    CALL(check_device(a->q, blocks * kBlock8, name));
-    return check_device(a->e, blocks, name);
+    CALL(check_device(s, a->q, blocks * kBlock8, 16, name));
+    return check_device(s, a->e, blocks, 1, name);
 }
 
-int check_rules(const spdp_rules *r, int64_t rows, int64_t n)
+int check_rules(const spdp_state *s, const spdp_rules *r, int64_t rows, int64_t n)
 {
     if (r->rows != rows || r->n_words != n)
         return fail(SPDP_E_ARG, "rules for %lld x %d scores, not %lld x %lld", (long long)r->rows,
@@ -1134,9 +1146,9 @@ int check_rules(const spdp_rules *r, int64_t rows, int64_t n)
     if (rows == 0) return SPDP_OK;
     if (r->doc_off) {
         if (!r->penalties) return fail(SPDP_E_ARG, "rules: listed words without penalties");
-        CALL(check_device(r->doc_off, (rows + 1) * 8, "rules: doc_off"));
-        CALL(check_device(r->words, r->n_listed * 4, "rules: words"));
-        CALL(check_device(r->penalties, rows * 12, "rules: penalties"));
+        CALL(check_device(s, r->doc_off, (rows + 1) * 8, 8, "rules: doc_off"));
+        CALL(check_device(s, r->words, r->n_listed * 4, 4, "rules: words"));
+        CALL(check_device(s, r->penalties, rows * 12, 4, "rules: penalties"));
     } else if (r->words || r->penalties) {
         return fail(SPDP_E_ARG, "rules: words and penalties need doc_off");
     }
@@ -1154,8 +1166,10 @@ int check_rules(const spdp_rules *r, int64_t rows, int64_t n)
             continue;
         }
         if (t.entries < 1) return fail(SPDP_E_ARG, "%s has no rows", t.name);
-        CALL(check_device(t.table, t.entries * t.width * 4, t.name));
-        if (t.of) CALL(check_device(t.of, rows * 4, t.name_of));
+        if (t.entries > (INT64_MAX >> 4) / t.width)
+            return fail(SPDP_E_ARG, "%s: more elements than memory holds", t.name);
+        CALL(check_device(s, t.table, t.entries * t.width * 4, 4, t.name));
+        if (t.of) CALL(check_device(s, t.of, rows * 4, 4, t.name_of));
     }
     return SPDP_OK;
 }
@@ -1167,32 +1181,32 @@ int check_blocks(int64_t blocks)
     return SPDP_OK;
 }
 
-int check_work(const void *work, int64_t have, int64_t need)
+int check_work(const spdp_state *s, const void *work, int64_t have, int64_t need)
 {
     if (have < need)
         return fail(SPDP_E_ARG, "a workspace of %lld bytes, not %lld", (long long)need,
                     (long long)have);
     if (!aligned16(work)) return fail(SPDP_E_ARG, "the workspace is not 16-byte aligned");
-    return check_device(work, need, "work");
+    return check_device(s, work, need, 16, "work");
 }
 
-int check_take(int32_t k, int64_t rows, const int32_t *word, const float *value)
+int check_take(const spdp_state *s, int32_t k, int64_t rows, const int32_t *word, const float *value)
 {
     if (k < 1 || k > SPDP_MAX_TAKE)
         return fail(SPDP_E_ARG, "k must be in [1, %d]", SPDP_MAX_TAKE);
-    CALL(check_device(word, rows * k * 4, "word"));
-    return check_device(value, rows * k * 4, "value");
+    CALL(check_device(s, word, rows * k * 4, 4, "word"));
+    return check_device(s, value, rows * k * 4, 4, "value");
 }
 
-int check_draws(int32_t draws, double temperature, int64_t rows, const double *u,
+int check_draws(const spdp_state *s, int32_t draws, double temperature, int64_t rows, const double *u,
                 const int32_t *word, const float *logp)
 {
     if (draws < 0 || draws > 1 << 20) return fail(SPDP_E_ARG, "draws must be in [0, 2^20]");
     if (!(temperature >= 1e-6 && temperature <= 1e6))
         return fail(SPDP_E_ARG, "temperature must be in [1e-6, 1e6]");
-    if (u) CALL(check_device(u, rows * draws * 8, "u"));
-    CALL(check_device(word, rows * draws * 4, "word"));
-    return check_device(logp, rows * draws * 4, "logp");
+    if (u) CALL(check_device(s, u, rows * draws * 8, 8, "u"));
+    CALL(check_device(s, word, rows * draws * 4, 4, "word"));
+    return check_device(s, logp, rows * draws * 4, 4, "logp");
 }
 
 // The rules of the rows from `row` on.
@@ -1224,11 +1238,10 @@ int spdp_pack8(spdp_state *s, const void *x, int32_t type, int64_t ld, const spd
     if (!s) return fail(SPDP_E_ARG, "state is NULL");
     if (type != SPDP_F64 && type != SPDP_F32)
         return fail(SPDP_E_ARG, "rows to pack are SPDP_F64 or SPDP_F32");
-    CALL(check_rows8(out, "out"));
+    CALL(check_rows8(s, out, "out"));
     int64_t bytes = 0;
     CALL(matrix_bytes(out->rows, out->cols, ld, type, "x", &bytes));
-    if ((uintptr_t)x % type_size(type) != 0) return fail(SPDP_E_ARG, "x is misaligned");
-    CALL(check_device(x, bytes, "x"));
+    CALL(check_device(s, x, bytes, (int)type_size(type), "x"));
     CALL(check_blocks(out->rows * blocks8(out->cols) / 4 + 1));
     OnDevice on(s->device);
     HIP_TRY(on.error());
@@ -1240,12 +1253,12 @@ int spdp_product8(spdp_state *s, const spdp_rows8 *a, const spdp_rows8 *b, int32
                   void *c, int32_t type, int64_t ld)
 {
     if (!s) return fail(SPDP_E_ARG, "state is NULL");
-    CALL(check_rows8(a, "a"));
-    CALL(check_rows8(b, "b"));
+    CALL(check_rows8(s, a, "a"));
+    CALL(check_rows8(s, b, "b"));
     if (a->cols != b->cols)
         return fail(SPDP_E_ARG, "rows of %d and %d columns", a->cols, b->cols);
     if (b->rows == 0) return SPDP_OK;
-    CALL(check_scores(c, ld, type, a->rows, b->rows, "c"));
+    CALL(check_scores(s, c, ld, type, a->rows, b->rows, "c"));
     CALL(check_blocks((a->rows + 15) / 16 * ((b->rows + 15) / 16)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
@@ -1259,9 +1272,9 @@ int spdp_adjust(spdp_state *s, const void *x, int64_t ldx, void *y, int64_t ldy,
     if (!s) return fail(SPDP_E_ARG, "state is NULL");
     if (!rules) return fail(SPDP_E_ARG, "rules is NULL");
     const int64_t rows = rules->rows, n = rules->n_words;
-    CALL(check_scores(x, ldx, type, rows, n, "x"));
-    CALL(check_scores(y, ldy, type, rows, n, "y"));
-    CALL(check_rules(rules, rows, n));
+    CALL(check_scores(s, x, ldx, type, rows, n, "x"));
+    CALL(check_scores(s, y, ldy, type, rows, n, "y"));
+    CALL(check_rules(s, rules, rows, n));
     if (rows > 0 && (x != y || ldx != ldy)) {
         const int64_t size = type_size(type);
         const uintptr_t x0 = (uintptr_t)x, x1 = x0 + ((rows - 1) * ldx + n) * size;
@@ -1290,10 +1303,10 @@ int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t row
              void *work, int64_t work_bytes)
 {
     if (!s) return fail(SPDP_E_ARG, "state is NULL");
-    CALL(check_scores(x, ld, type, rows, n_words, "x"));
-    if (rules) CALL(check_rules(rules, rows, n_words));
-    CALL(check_take(k, rows, word, value));
-    CALL(check_work(work, work_bytes, words_work(rows, n_words, k)));
+    CALL(check_scores(s, x, ld, type, rows, n_words, "x"));
+    if (rules) CALL(check_rules(s, rules, rows, n_words));
+    CALL(check_take(s, k, rows, word, value));
+    CALL(check_work(s, work, work_bytes, words_work(rows, n_words, k)));
     CALL(check_blocks(words_blocks(rows, n_words)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
@@ -1308,10 +1321,10 @@ int spdp_draw(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t ro
               void *work, int64_t work_bytes)
 {
     if (!s) return fail(SPDP_E_ARG, "state is NULL");
-    CALL(check_scores(x, ld, type, rows, n_words, "x"));
-    if (rules) CALL(check_rules(rules, rows, n_words));
-    CALL(check_draws(draws, temperature, rows, u, word, logp));
-    CALL(check_work(work, work_bytes, words_work(rows, n_words, 0)));
+    CALL(check_scores(s, x, ld, type, rows, n_words, "x"));
+    if (rules) CALL(check_rules(s, rules, rows, n_words));
+    CALL(check_draws(s, draws, temperature, rows, u, word, logp));
+    CALL(check_work(s, work, work_bytes, words_work(rows, n_words, 0)));
     CALL(check_blocks(words_blocks(rows, n_words)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
@@ -1339,20 +1352,20 @@ int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
                  int64_t work_bytes)
 {
     if (!s || !answer) return fail(SPDP_E_ARG, "null argument");
-    CALL(check_rows8(docs, "docs"));
-    CALL(check_rows8(words, "words"));
+    CALL(check_rows8(s, docs, "docs"));
+    CALL(check_rows8(s, words, "words"));
     if (docs->cols != words->cols)
         return fail(SPDP_E_ARG, "rows of %d and %d columns", docs->cols, words->cols);
     const spdp_answer a = *answer;
     const int64_t D = docs->rows, V = words->rows;
     if (V < 1) return fail(SPDP_E_ARG, "no words");
     const bool kept = a.scores != nullptr;
-    if (kept) CALL(check_scores(a.scores, a.ld, a.type, D, V, "scores"));
+    if (kept) CALL(check_scores(s, a.scores, a.ld, a.type, D, V, "scores"));
     else if (a.type != SPDP_F32 && a.type != SPDP_F16 && a.type != SPDP_BF16)
         return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
-    if (rules) CALL(check_rules(rules, D, V));
-    if (a.k != 0) CALL(check_take(a.k, D, a.top_word, a.top_value));
-    if (a.draws != 0) CALL(check_draws(a.draws, a.temperature, D, a.u, a.draw_word, a.draw_logp));
+    if (rules) CALL(check_rules(s, rules, D, V));
+    if (a.k != 0) CALL(check_take(s, a.k, D, a.top_word, a.top_value));
+    if (a.draws != 0) CALL(check_draws(s, a.draws, a.temperature, D, a.u, a.draw_word, a.draw_logp));
     if (D == 0) return SPDP_OK;
     const bool choose = a.k > 0 || a.draws > 0;
     auto need = [&](int64_t rows) {
@@ -1369,7 +1382,7 @@ int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
         }
         rows = low > kPredictTile ? low - low % kPredictTile : low;
     }
-    CALL(check_work(work, work_bytes, need(rows)));
+    CALL(check_work(s, work, work_bytes, need(rows)));
     CALL(check_blocks(words_blocks(rows, V)));
     CALL(check_blocks((rows + 15) / 16 * ((V + 15) / 16)));
     OnDevice on(s->device);

@@ -474,10 +474,6 @@ hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld
     const int32_t nb = blocks8(a.cols), held = nb < kLdsBlocks / FD ? nb : kLdsBlocks / FD;
     const Shares s = shares_of(a.rows, b.rows, FD);
     const int64_t per = (s.tiles_d * s.ranges + 7) / 8;
-    static const hipError_t room = hipFuncSetAttribute(
-        reinterpret_cast<const void *>(&k_product8<T, LOG, FD, STREAM>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBlocks * 4096);
-    if (room != hipSuccess) return room;
     hipLaunchKernelGGL((k_product8<T, LOG, FD, STREAM>), dim3((unsigned)(per * 8)), dim3(512),
                        held * FD * 4096, st, a.q, a.e, (int32_t)a.rows, b.q, b.e, (int32_t)b.rows,
                        nb, (T *)c, ld, (int32_t)s.tiles_d, (int32_t)s.ranges, (int32_t)s.rounds);

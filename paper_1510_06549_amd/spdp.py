@@ -538,6 +538,8 @@ class Rules:
                  bias_of=None, mask=None, mask_of=None):
         i32, f32 = "torch.int32", "torch.float32"
         tables = [0 if t is None else t.shape[0] for t in (bias, mask)]
+        if any(t is not None and n == 0 for t, n in zip((bias, mask), tables)):
+            raise ValueError("a table without rows")
         listed = 0 if words is None else words.shape[0]
         self.kept = (doc_off, words, penalties, bias, bias_of, mask, mask_of)
         self.rows, self.n_words = rows, n_words

@@ -10,6 +10,8 @@ magnitudes (2^-24, or a cut of the last place); its logarithm adds 2^-22 of itse
 hardware's base-2 logarithm, its scaling and their roundings); then half a step of the
 output's type.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -517,6 +519,62 @@ def test_no_rows_and_no_draws(state):
                    e(0, 50, dtype=torch.float32))
 
 
+@pytest.mark.parametrize("type", ["f32", "f16"])
+def test_long_rows(state, type):
+    """Rows of more chunks than a wavefront has lanes, with rules."""
+    V, n, k = 1200001, 64, 200
+    say(f"top and draw of 2 x {V} {type}")
+    rng = np.random.default_rng(21)
+    x = _scores(rng, 2, V, TYPES[type])
+    x[1, :700000] = -np.inf
+    mask = np.full((1, -(-V // 32)), 0x5DB5D5B7, np.uint32)
+    docs = [rng.integers(0, V, 3000), np.array([5, V - 1, V - 1])]
+    pen = np.array([[1.5, 0.5, 0.25]] * 2, np.float32)
+    r = sp.Rules(2, V, doc_off=dev(np.array([0, 3000, 3003])),
+                 words=dev(np.concatenate(docs).astype(np.int32)), penalties=dev(pen),
+                 mask=dev(mask.view(np.int32)))
+    allowed = np.unpackbits(mask.view(np.uint8), axis=1, bitorder="little")[:, :V].astype(bool)
+    xo = ow.adjusted(x.float().cpu().numpy(), docs, pen, None, np.repeat(allowed, 2, 0))
+    word = torch.empty((2, k), dtype=torch.int32, device="cuda")
+    value = torch.empty((2, k), device="cuda")
+    sp.spdp_top(state.h, x, word, value, work_for(2, V, k), rules=r)
+    order = [np.lexsort((np.arange(V), -row.astype(np.float64)))[:k] for row in xo]
+    np.testing.assert_array_equal(word.cpu().numpy(), order)
+    np.testing.assert_array_equal(value.cpu().numpy(), np.take_along_axis(xo, np.array(order), 1))
+    u = rng.random((2, n))
+    u[:, 0], u[:, 1] = 1.0, 0.0
+    word = torch.empty((2, n), dtype=torch.int32, device="cuda")
+    logp = torch.empty((2, n), device="cuda")
+    sp.spdp_draw(state.h, x, word, logp, work_for(2, V), u=dev(u), rules=r)
+    _check_draws(word.cpu().numpy(), logp.cpu().numpy(), xo, u, 1.0)
+
+
+@pytest.mark.parametrize("m,n", [(3, 100), (70, 200)])
+def test_product_many_columns(state, m, n):
+    """More columns than the documents' tile holds at a time."""
+    say(f"product {m} x {n} x 5000")
+    rng = np.random.default_rng(22)
+    a8, a = _packed(rng, m, 5000, 1.0)
+    b8, b = _packed(rng, n, 5000, 1.0)
+    for log in (False, True):
+        out = torch.empty((m, n), device="cuda")
+        sp.spdp_product8(state.h, a8, b8, out, log=log)
+        _check_product(out.double().cpu().numpy(), a, b, log, torch.float32)
+
+
+@pytest.mark.parametrize("n", [63, 64, 1000])
+def test_product_does_not_depend_on_the_batch(state, n):
+    say(f"product: rows alone and together, {n} words")
+    rng = np.random.default_rng(23)
+    a8, _ = _packed(rng, 300, 700, 2.0)
+    b8, _ = _packed(rng, n, 700, 2.0)
+    whole = sp.spdp_product8(state.h, a8, b8, torch.empty((300, n), device="cuda"), log=True)
+    for i, j in ((0, 1), (5, 6), (0, 16), (3, 20), (0, 40), (100, 164), (7, 97), (11, 300)):
+        part = sp.Rows8(a8.q[i:j], a8.e[i:j], 700)
+        out = torch.empty((j - i, n), device="cuda")
+        assert torch.equal(sp.spdp_product8(state.h, part, b8, out, log=True), whole[i:j]), (i, j)
+
+
 # ---------------------------------------------------------------------------
 # refusals that need a device
 # ---------------------------------------------------------------------------
@@ -549,13 +607,29 @@ def test_refusals_on_device(state):
         words=torch.zeros(1, dtype=torch.int32, device="cuda")), x)
     refused("without its table", sp.spdp_adjust, state.h, x, sp.Rules(
         4, 100, mask_of=torch.zeros(4, dtype=torch.int32, device="cuda")), x)
+    with pytest.raises(ValueError):  # (torch has no address for it)
+        sp.Rules(4, 100, bias=x[:0])
     L = sp.lib()
+    none = sp._Rules(rows=4, n_words=100, bias=x.data_ptr())
+    assert L.spdp_adjust(state.h, x.data_ptr(), 100, x.data_ptr(), 100, sp.SPDP_F32,
+                         ctypes.addressof(none)) == sp.SPDP_E_ARG
+    assert "rules: bias has no rows" in sp.spdp_last_error()
+    # misaligned arrays of the rules
+    off = torch.zeros(64, dtype=torch.int32, device="cuda")
+    for field in ("doc_off", "words", "penalties", "bias", "mask"):
+        c = sp._Rules(rows=4, n_words=100, n_bias=1, n_masks=1, n_listed=4)
+        if field in ("doc_off", "words", "penalties"):
+            for f in ("doc_off", "words", "penalties"):
+                setattr(c, f, x.data_ptr())
+        setattr(c, field, off.data_ptr() + 2)
+        assert L.spdp_adjust(state.h, x.data_ptr(), 100, x.data_ptr(), 100, sp.SPDP_F32,
+                             ctypes.addressof(c)) == sp.SPDP_E_ARG
+        assert f"{field} is misaligned" in sp.spdp_last_error()
     host = np.zeros((4, 100), np.float32)
     assert L.spdp_adjust(state.h, host.ctypes.data, 100, x.data_ptr(), 100, sp.SPDP_F32,
                          r.ref) == sp.SPDP_E_ARG and "x is not device" in sp.spdp_last_error()
     # rows far past the allocation
     big = sp._Rules(rows=1 << 30, n_words=100)
-    import ctypes
     assert L.spdp_adjust(state.h, x.data_ptr(), 100, x.data_ptr(), 100, sp.SPDP_F32,
                          ctypes.addressof(big)) == sp.SPDP_E_ARG
     assert "run past its allocation" in sp.spdp_last_error()
