@@ -55,8 +55,16 @@ __device__ __forceinline__ uint32_t order_of(float x)
     return x > -__builtin_inff() ? order : 0;  // neither -inf nor NaN
 }
 
-__device__ __forceinline__ u64 key_of(uint32_t order, int64_t w)
+// The least score with this order; the lowest finite one for 0.
+__device__ __forceinline__ float score_of_order(uint32_t order)
 {
+    const uint32_t b = order & 0x80000000u ? order & 0x7FFFFFFFu : ~order;
+    return order ? __uint_as_float(b) : -3.402823466e+38f;
+}
+
+__device__ __forceinline__ u64 key_of(float x, int64_t w)
+{
+    const uint32_t order = order_of(x);
     return order ? (u64)order << 32 | (uint32_t)~(uint32_t)w : 0;
 }
 
@@ -254,10 +262,8 @@ __device__ __forceinline__ void rank_keys(Kept &kept, int n, int k, F put)
 
 __device__ __forceinline__ void put_top(u64 key, int32_t *word, float *value)
 {
-    const uint32_t order = (uint32_t)(key >> 32);
     *word = key ? (int32_t)~(uint32_t)key : -1;
-    *value = key ? __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order)
-                 : -__builtin_inff();
+    *value = key ? score_of_order((uint32_t)(key >> 32)) : -__builtin_inff();
 }
 
 // One workgroup per part of a row: `words` words, a chunk at a time.  What could be among
@@ -295,7 +301,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     const bool grouped = threads >= k, empty = (int)(threadIdx.x / group * group) >= threads;
     const int wave = threadIdx.x >> 6;
     int n = 0;           // keys kept
-    uint32_t mine = 0;   // largest order that this thread has seen
+    float mine = -__builtin_inff();  // largest score that this thread has seen
     u64 bound = 1;       // keys below are not among the k best
     auto raise = [&](const uint32_t (&w)[kTopWaves]) {
         const uint32_t least = group <= 64    ? min(min(w[0], w[1]), min(w[2], w[3]))
@@ -307,32 +313,28 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     int turn = 0;
     for (int64_t w0 = first; w0 < end; w0 += C::kWords, turn ^= 1) {
         if (r.n_words > 0) C::count(r, w0, listed);
-        uint32_t order[C::U][C::N];
+        float v[C::U][C::N];
 #pragma unroll
         for (int u = 0; u < C::U; ++u) {
-            float v[C::N];
-            c.scores(r, w0, end, listed, u, v);
+            c.scores(r, w0, end, listed, u, v[u]);
 #pragma unroll
-            for (int i = 0; i < C::N; ++i) {
-                order[u][i] = order_of(v[i]);
-                mine = order[u][i] > mine ? order[u][i] : mine;
-            }
+            for (int i = 0; i < C::N; ++i) mine = fmaxf(mine, v[u][i]);
         }
         if (w0 + C::kWords < end) c.request(x, w0 + C::kWords, end);
-        const uint32_t least = least_largest(mine, group, empty);
+        const uint32_t least = least_largest(order_of(mine), group, empty);
         if ((threadIdx.x & 63) == 0) wave_least[turn][wave] = least;
         if (w0 == first) {  // (later chunks go by the bound of the ones before)
             __syncthreads();
             raise(wave_least[turn]);
         }
-        const uint32_t low = (uint32_t)(bound >> 32) > 1 ? (uint32_t)(bound >> 32) : 1;
-        uint32_t pass = 0;
+        // (at least the lowest finite score, so that neither -inf nor NaN passes)
+        const float low = score_of_order((uint32_t)(bound >> 32));
+        int pass = 0;
 #pragma unroll
         for (int u = 0; u < C::U; ++u)
 #pragma unroll
-            for (int i = 0; i < C::N; ++i)
-                pass |= (uint32_t)(order[u][i] >= low) << (u * C::N + i);
-        int passing, to = places(__builtin_popcount(pass), n, wave_pass[turn], passing);
+            for (int i = 0; i < C::N; ++i) pass += v[u][i] >= low;
+        int passing, to = places(pass, n, wave_pass[turn], passing);
         raise(wave_least[turn]);
         if (n + passing <= kKeys) {
             if (pass) {
@@ -340,8 +342,8 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
                 for (int u = 0; u < C::U; ++u)
 #pragma unroll
                     for (int i = 0; i < C::N; ++i)
-                        if (pass >> (u * C::N + i) & 1u)
-                            kept.key[to++] = key_of(order[u][i], w0 + C::at(u) + i);
+                        if (v[u][i] >= low)
+                            kept.key[to++] = key_of(v[u][i], w0 + C::at(u) + i);
             }
             n += passing;
             if (r.n_words > 0) __syncthreads();  // (before the next chunk's words are counted)
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
                 int more = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    key[e] = key_of(order[u][i + e], w0 + C::at(u) + i + e);
+                    key[e] = key_of(v[u][i + e], w0 + C::at(u) + i + e);
                     more += key[e] >= bound;
                 }
                 int at = places(more, n, wave_pass[0], passing);
