@@ -71,6 +71,7 @@ __device__ __forceinline__ u64 key_of(float x, int64_t w)
 constexpr int kTopThreads = 256;
 constexpr int kTopWaves = kTopThreads / 64;
 constexpr int kKeys = 2048;  // kept at a time in LDS
+constexpr int kKeysEach = kKeys / kTopThreads;
 
 struct Kept {  // LDS
     u64 key[kKeys];
@@ -126,31 +127,31 @@ __device__ __forceinline__ int prefix(int v)
     return v;
 }
 
-// Of `group` lanes each (a power of 2, groups in a row) the largest value, and of the groups
-// that are not empty the least of these; for 64 lanes and more, the wavefront's largest.
-__device__ __forceinline__ uint32_t least_largest(uint32_t v, int group, bool empty)
+// A bound that at least k (<= kTopThreads) of the threads' values reach, and not many more:
+// found a bit at a time, over the bits that not all values have alike, until it is reached by
+// at most k / 8 more.  All threads call it, with a barrier between two calls; there is
+// one in it.  Every wavefront counts for itself, so that no barrier is needed for a bit.
+__device__ __forceinline__ uint32_t reached(uint32_t mine, int k, uint32_t (&value)[kTopThreads])
 {
-    const auto step = [&](int d, uint32_t o) { v = d < group ? max(v, o) : min(v, o); };
-    if (group == 1) v = empty ? ~0u : v;
-    step(1, other<1>(v));
-    if (group == 2) v = empty ? ~0u : v;
-    step(2, other<2>(v));
-    if (group == 4) v = empty ? ~0u : v;
-    step(4, other<4>(v));
-    if (group == 8) v = empty ? ~0u : v;
-    step(8, other<8>(v));
-    if (group == 16) v = empty ? ~0u : v;
-    uint32_t row[4];
-    for (int i = 0; i < 4; ++i) row[i] = __builtin_amdgcn_readlane((int)v, 16 * i);
-    uint32_t a = group > 16 ? max(row[0], row[1]) : min(row[0], row[1]);
-    uint32_t b = group > 16 ? max(row[2], row[3]) : min(row[2], row[3]);
-    const u64 none = __ballot(empty);
-    if (group == 32) {
-        a = none & 1 ? ~0u : a;
-        b = none >> 32 & 1 ? ~0u : b;
+    static_assert(kTopThreads == 256, "four values a lane");
+    typedef uint32_t quad __attribute__((ext_vector_type(4)));
+    value[threadIdx.x] = mine;
+    __syncthreads();
+    const quad v = reinterpret_cast<const quad *>(value)[threadIdx.x & 63];
+    uint32_t bound = ~wave_or(~(v[0] & v[1] & v[2] & v[3]));
+    uint32_t differ = wave_or(v[0] | v[1] | v[2] | v[3]) ^ bound;
+    while (differ) {
+        const uint32_t high = 1u << (31 - __builtin_clz(differ)), t = bound | high;
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reach += __builtin_popcountll(__ballot(v[i] >= t));
+        if (reach >= k) {
+            bound = t;
+            if (reach <= k + k / 8) break;
+        }
+        differ ^= high;
     }
-    a = group > 32 ? max(a, b) : min(a, b);
-    return group == 64 && (none & 1) ? ~0u : a;
+    return bound;
 }
 
 // Places for `mine` keys of each thread, in the threads' order: the thread's first place
@@ -169,26 +170,56 @@ __device__ __forceinline__ int places(int mine, int before, int (&slot)[kTopWave
     return before + upto - mine;
 }
 
-// Cuts the n keys (k < n <= kKeys) down to the k largest, in any order, and returns how many
-// there are (less than k where there are not so many but 0); least is a bound that only
-// they reach: the largest that k keys reach, found two bits at a time, over the bits that
-// not all keys have alike, until exactly k reach it.  All threads call it, behind a
-// barrier; there is one before it returns.
-__device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
+// The keys of each thread, of n; 0 for none.
+__device__ __forceinline__ void for_keys(const Kept &kept, int n, u64 (&key)[kKeysEach])
 {
-    constexpr int kPer = kKeys / kTopThreads;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 key[kPer];
-    u64 any = 0, all = ~0ull;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < kKeysEach; ++i) {
         const int at = threadIdx.x + i * kTopThreads;
         key[i] = at < n ? kept.key[at] : 0;
-        if (at < n) {
+    }
+}
+
+// Keeps of the keys that each thread holds those that reach the bound (> 0), and returns how
+// many there are.  All threads call it; there is a barrier before the keys are written and
+// one before it returns.
+__device__ __forceinline__ int keep_keys(Kept &kept, const u64 (&key)[kKeysEach], u64 bound)
+{
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kKeysEach; ++i) mine += key[i] >= bound;
+    __syncthreads();
+    int total, to = places(mine, 0, kept.in_wave[0][0], total);
+#pragma unroll
+    for (int i = 0; i < kKeysEach; ++i)
+        if (key[i] >= bound) kept.key[to++] = key[i];
+    __syncthreads();
+    return total;
+}
+
+// So many keys for the k best are ranked rather than brought further down.
+__device__ __forceinline__ int enough_keys(int k)
+{
+    const int n = k + k / 4 < 64 ? 64 : k + k / 4;
+    return n < kTopThreads ? n : kTopThreads;
+}
+
+// Cuts the n keys (kTopThreads < n <= kKeys, none 0) down to at least k and no more than are
+// enough, the k largest among them, in any order, and returns how many; least is a bound
+// that only they reach, found two bits at a time, over the bits that not all keys have
+// alike.  All threads call it, behind a barrier; there is one before it returns.
+__device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 key[kKeysEach];
+    for_keys(kept, n, key);
+    u64 any = 0, all = ~0ull;
+#pragma unroll
+    for (int i = 0; i < kKeysEach; ++i)
+        if ((int)threadIdx.x + i * kTopThreads < n) {
             any |= key[i];
             all &= key[i];
         }
-    }
     any = wave_or(any);
     all = ~wave_or(~all);
     __syncthreads();
@@ -208,7 +239,7 @@ __device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
         const u64 t[3] = {bound | high | low, bound | high, bound | low};
         int reach[3] = {0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
+        for (int i = 0; i < kKeysEach; ++i) {
             if (i * kTopThreads >= n) break;
 #pragma unroll
             for (int j = 0; j < 3; ++j) reach[j] += __builtin_popcountll(__ballot(key[i] >= t[j]));
@@ -222,21 +253,11 @@ __device__ __forceinline__ int cut_keys(Kept &kept, int n, int k, u64 &least)
         }
         const int j = reach[0] >= k ? 0 : reach[1] >= k ? 1 : low && reach[2] >= k ? 2 : 3;
         if (j < 3) bound = t[j];
-        if (j < 3 && reach[j] == k) break;
+        if (j < 3 && reach[j] <= enough_keys(k)) break;
         differ = rest ^ low;
     }
-    bound = bound ? bound : 1;
-    int mine = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) mine += key[i] >= bound;
-    __syncthreads();
-    int total, to = places(mine, 0, kept.in_wave[0][0], total);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (key[i] >= bound) kept.key[to++] = key[i];
-    __syncthreads();
     least = bound;
-    return total;
+    return keep_keys(kept, key, bound);
 }
 
 // Calls put(rank, key) for the k largest of the n keys, n <= kTopThreads: a key's rank is
@@ -268,9 +289,9 @@ __device__ __forceinline__ void put_top(u64 key, int32_t *word, float *value)
 
 // One workgroup per part of a row: `words` words, a chunk at a time.  What could be among
 // the k best is collected in LDS: scores at or above a bound that at least k of those seen
-// so far reach, namely the least of the largest scores that groups of threads have
-// seen, with at least k groups.  The bound rises as the groups see more, so that after
-// the first chunk few scores pass.  Where the collection would overflow (many ties), it
+// so far reach, namely the largest scores that k of the threads have seen.  Of 256 threads
+// that have seen m scores each about k (1 + k / 512) reach the bound; it rises each time that
+// the threads have seen twice as many, so that few scores pass.  Where the collection would overflow (many ties), it
 // is cut down to its k best, again and again.
 template <typename T>
 __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict__ x, int64_t ld,
@@ -283,7 +304,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     using C = Chunk<T, kTopThreads, 16>;
     __shared__ typename C::Listed listed;
     __shared__ Kept kept;
-    __shared__ uint32_t wave_least[2][kTopWaves];
+    __shared__ alignas(16) uint32_t largest[kTopThreads];
     __shared__ int wave_pass[2][kTopWaves];
     const int64_t row = blockIdx.x / (uint32_t)parts;
     const int64_t first = (int64_t)(blockIdx.x % (uint32_t)parts) * words;
@@ -292,26 +313,11 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     C c;
     c.request(x, first, end);
     const RowRules r = row_rules(rules, row);
-    // threads that hold words of the first chunk, and the largest groups of which there
-    // are k (no group: fewer than k threads; then every score passes)
-    const int64_t holding = (end - first + C::N - 1) / C::N;
-    const int threads = holding < kTopThreads ? (int)holding : kTopThreads;
-    int group = 1;
-    while (group < kTopThreads && (threads + 2 * group - 1) / (2 * group) >= k) group *= 2;
-    const bool grouped = threads >= k, empty = (int)(threadIdx.x / group * group) >= threads;
-    const int wave = threadIdx.x >> 6;
     int n = 0;           // keys kept
     float mine = -__builtin_inff();  // largest score that this thread has seen
     u64 bound = 1;       // keys below are not among the k best
-    auto raise = [&](const uint32_t (&w)[kTopWaves]) {
-        const uint32_t least = group <= 64    ? min(min(w[0], w[1]), min(w[2], w[3]))
-                               : group == 128 ? min(max(w[0], w[1]), max(w[2], w[3]))
-                                              : max(max(w[0], w[1]), max(w[2], w[3]));
-        const u64 b = (u64)least << 32;
-        bound = grouped && b > bound ? b : bound;
-    };
-    int turn = 0;
-    for (int64_t w0 = first; w0 < end; w0 += C::kWords, turn ^= 1) {
+    int chunk = 0;
+    for (int64_t w0 = first; w0 < end; w0 += C::kWords, ++chunk) {
         if (r.n_words > 0) C::count(r, w0, listed);
         float v[C::U][C::N];
 #pragma unroll
@@ -321,11 +327,9 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
             for (int i = 0; i < C::N; ++i) mine = fmaxf(mine, v[u][i]);
         }
         if (w0 + C::kWords < end) c.request(x, w0 + C::kWords, end);
-        const uint32_t least = least_largest(order_of(mine), group, empty);
-        if ((threadIdx.x & 63) == 0) wave_least[turn][wave] = least;
-        if (w0 == first) {  // (later chunks go by the bound of the ones before)
-            __syncthreads();
-            raise(wave_least[turn]);
+        if ((chunk & (chunk + 1)) == 0) {  // chunks 0, 1, 3, 7, ..: twice as much seen
+            const u64 b = (u64)reached(order_of(mine), k, largest) << 32;
+            bound = b > bound ? b : bound;
         }
         // (at least the lowest finite score, so that neither -inf nor NaN passes)
         const float low = score_of_order((uint32_t)(bound >> 32));
@@ -334,8 +338,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
         for (int u = 0; u < C::U; ++u)
 #pragma unroll
             for (int i = 0; i < C::N; ++i) pass += v[u][i] >= low;
-        int passing, to = places(pass, n, wave_pass[turn], passing);
-        raise(wave_least[turn]);
+        int passing, to = places(pass, n, wave_pass[chunk & 1], passing);
         if (n + passing <= kKeys) {
             if (pass) {
 #pragma unroll
@@ -376,6 +379,13 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
         __syncthreads();
     }
     __syncthreads();
+    // the bound by all scores, for the keys from before it rose (ranks of few keys cost less)
+    if (chunk > 1 && n > enough_keys(k)) {
+        const u64 b = (u64)reached(order_of(mine), k, largest) << 32;
+        u64 key[kKeysEach];
+        for_keys(kept, n, key);
+        n = keep_keys(kept, key, b > 1 ? b : 1);
+    }
     if (n > kTopThreads) {
         u64 least;
         n = cut_keys(kept, n, k, least);
@@ -393,38 +403,64 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     }
 }
 
-// One workgroup per row: the k best of its parts' keys, n in all.
-__global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict__ best, int64_t n,
-                                                          int32_t k, int32_t *__restrict__ word,
+// One workgroup per row: the k best of its parts' keys, k of each part in order.  The last
+// of a run of four keys is reached by all four, so that what (k + 3) / 4 of the threads' runs
+// reach bounds the k best; the keys that reach it are few beside all (k and less than four
+// of each part's, where no thread has more than one run).
+__global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict__ best,
+                                                          int32_t parts, int32_t k,
+                                                          int32_t *__restrict__ word,
                                                           float *__restrict__ value)
 {
     __shared__ Kept kept;
+    __shared__ alignas(16) uint32_t largest[kTopThreads];
     const int64_t row = blockIdx.x;
+    const int n = parts * k;
     best += row * n;
+    const int run = k < 4 ? 1 : 4, runs = k / run;  // (of a part; keys behind them are in none)
+    uint32_t mine = 0;
+    for (int i = threadIdx.x; i < parts * runs; i += kTopThreads) {
+        const int part = i / runs;
+        const u64 key = best[part * k + (i - part * runs) * run + run - 1];
+        const uint32_t order = (uint32_t)(key >> 32);
+        mine = mine > order ? mine : order;
+    }
+    u64 bound = (u64)reached(mine, (k + run - 1) / run, largest) << 32;
+    bound = bound ? bound : 1;
+    constexpr int kEach = 4;  // keys a thread at a time
+    static_assert(kEach * kTopThreads <= kKeys / 2, "room after every cut");
     int have = 0;
-    for (int64_t from = 0; from < n;) {
-        const int take = (int)(n - from < kKeys - have ? n - from : kKeys - have);
-        for (int i = threadIdx.x; i < take; i += kTopThreads) kept.key[have + i] = best[from + i];
-        from += take;
-        have += take;
+    for (int from = 0; from < n; from += kEach * kTopThreads) {
+        u64 key[kEach];
+        int more = 0, total;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = from + i * kTopThreads + threadIdx.x;
+            key[i] = at < n ? best[at] : 0;
+            more += key[i] >= bound;
+        }
+        int to = places(more, have, kept.in_wave[0][0], total);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (key[i] >= bound) kept.key[to++] = key[i];
+        have += total;
         __syncthreads();
-        if (have > kTopThreads) {
+        if (have > kKeys / 2) {
             u64 least;
             have = cut_keys(kept, have, k, least);
+            bound = least > bound ? least : bound;
         }
+    }
+    if (have > kTopThreads) {
+        u64 least;
+        have = cut_keys(kept, have, k, least);
     }
     word += row * k;
     value += row * k;
     rank_keys(kept, have, k, [&](int rank, u64 key) {
-        // (several places may hold no word: they share the rank behind the last word)
-        if (key) put_top(key, word + rank, value + rank);
+        put_top(key, word + rank, value + rank);
     });
-    __shared__ int found;
-    if (threadIdx.x == 0) found = 0;
-    __syncthreads();
-    if ((int)threadIdx.x < have && kept.key[threadIdx.x]) atomicAdd(&found, 1);
-    __syncthreads();
-    for (int t = found + threadIdx.x; t < k; t += kTopThreads) put_top(0, word + t, value + t);
+    for (int t = have + threadIdx.x; t < k; t += kTopThreads) put_top(0, word + t, value + t);
 }
 
 // ---------------------------------------------------------------------------
@@ -945,7 +981,7 @@ hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int
     });
     if (e != hipSuccess || s.parts == 1) return e;
     hipLaunchKernelGGL(k_top_join, dim3((unsigned)rows), dim3(kTopThreads), 0, st, best,
-                       s.parts * k, k, word, value);
+                       (int32_t)s.parts, k, word, value);
     return hipGetLastError();
 }
 
