@@ -471,14 +471,18 @@ __global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict_
 //
 // One pass over the scores leaves of every chunk its largest score, the sum of its
 // weights relative to that (the largest is then 1 in every chunk, and they do not
-// vanish beside the row's largest), and the sums up to the end of each of its blocks of
-// 64 words.  A draw is then one wavefront's work: the chunk among the chunks, the block
-// among its chunk's 128, the word among its block's 64 scores, by where the target
+// vanish beside the row's largest), the sums up to the end of each of its blocks of 64
+// words, and of each block's quarters the sum of 16 weights.  A wavefront then makes up to
+// 64 draws: the chunk among the chunks, each lane for its draw; the block among the
+// chunk's 128, all lanes for one draw after another; the quarter, each lane for its draw;
+// the word among the quarter's 16 scores, 16 lanes for a draw; each by where the target
 // falls between the sums up to one and up to the next.
 // ---------------------------------------------------------------------------
 constexpr int kDrawThreads = 512, kDrawPer = 16;
 constexpr int kDrawChunk = kDrawThreads * kDrawPer;
 constexpr int kBlockWords = 64, kBlocks = kDrawChunk / kBlockWords;  // two blocks a lane
+constexpr int kQuarterWords = 16, kQuarters = kDrawChunk / kQuarterWords;
+constexpr int kSums = kBlocks + kQuarters;  // of a chunk: up to each block, of each quarter
 
 struct Part {
     double top, sum;  // top: NaN where the chunk holds NaN or +inf
@@ -550,26 +554,41 @@ __device__ __forceinline__ double of_lane(double v, int lane)  // (the same lane
     return __builtin_bit_cast(double, (u64)hi << 32 | lo);
 }
 
-// Sum over the lanes up to and with each: within rows of 16 lanes, then a row's last lane
-// to the next row, then the lower half's last to the upper half.
-__device__ __forceinline__ double prefix(double v)
+// Sum over the lanes up to and with each, in its row of 16 lanes.
+__device__ __forceinline__ double row_prefix(double v)
 {
     v += moved<0x111>(v);  // shift right by 1, 2, 4, 8 in the row
     v += moved<0x112>(v);
     v += moved<0x114>(v);
     v += moved<0x118>(v);
+    return v;
+}
+
+// Sum over the lanes up to and with each: within rows of 16 lanes, then a row's last lane
+// to the next row, then the lower half's last to the upper half.
+__device__ __forceinline__ double prefix(double v)
+{
+    v = row_prefix(v);
     v += moved<0x142, 0xA>(v);  // lane 15 of a row to the next
     v += moved<0x143, 0xC>(v);  // lane 31 to the upper half
     return v;
 }
 
-// Sum over groups of 8 or 16 lanes, in each of their lanes.
+// Sums over a quarter's lanes (2 or 4, each with its part) in each of them; of those, over a
+// block's lanes (8 or 16).
 template <int LANES>
-__device__ __forceinline__ double group_sum(double v)
+__device__ __forceinline__ double quarter_sum(double v)
 {
-    v += moved<0xB1>(v);   // lane ^ 1
-    v += moved<0x4E>(v);   // lane ^ 2
-    v += moved<0x141>(v);  // the other four of eight
+    v += moved<0xB1>(v);                         // lane ^ 1
+    if constexpr (LANES == 4) v += moved<0x4E>(v);  // lane ^ 2
+    return v;
+}
+
+template <int LANES>
+__device__ __forceinline__ double block_sum(double v)
+{
+    if constexpr (LANES == 8) v += moved<0x4E>(v);
+    v += moved<0x141>(v);                            // the other four of eight
     if constexpr (LANES == 16) v += moved<0x140>(v);  // the other eight of sixteen
     return v;
 }
@@ -604,14 +623,18 @@ __device__ __forceinline__ void rising(const double (&share)[2], double (&upto)[
     upto[1] = fmax(upto[0], b);
 }
 
-// The lane whose sum is the first to exceed goal, else (goal infinite, or rounding) the
-// first that reaches the last sum, which has to be positive: in either case one with a
-// share.
-__device__ __forceinline__ int choose(double upto, double goal)
+// Of 64 rising sums, one a lane, with `last` the last: the first that exceeds this lane's
+// goal, else (rounding) the first that reaches the last one.
+__device__ __forceinline__ int first_past(double upto, double last, double goal)
 {
-    u64 lanes = __ballot(upto > goal);
-    if (!lanes) lanes = __ballot(upto == of_lane(upto, 63));
-    return __builtin_ctzll(lanes);
+    const bool past = last > goal;
+    int at = 0;
+#pragma unroll
+    for (int step = 32; step; step >>= 1) {
+        const double v = __shfl(upto, at + step - 1);
+        at += past ? (v > goal ? 0 : step) : (v < last ? step : 0);
+    }
+    return at;  // (<= 63)
 }
 
 // What a row's draws share.
@@ -669,144 +692,246 @@ __device__ __forceinline__ Law law_of(const Part *part, int32_t chunks, double s
     return law;
 }
 
-constexpr int kListed = 8;  // words of the document that a lane keeps
+// How often words are among a document's, which is looked up for a few words only.
+struct Times {  // LDS: a table by hash, of which a quarter stays empty
+    static constexpr int kSlots = 2048, kLogSlots = 11;
+    int32_t word[kSlots], count[kSlots];
 
-// `count` draws from d0 on of a row by one wavefront, a lane for each uniform and its
-// answer, one after another.
-template <typename T>
-__device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, const RowRules &r,
-                                           double scale, int32_t chunks, const Part *part,
-                                           const double *blocks, const Powers &powers, int64_t d0,
-                                           int32_t count, const double *__restrict__ u,
-                                           uint64_t seed, uint32_t step, int64_t draw0,
-                                           int32_t *__restrict__ word, float *__restrict__ logp)
-{
-    const int lane = threadIdx.x & 63;
-    int32_t listed[kListed];
+    // (longer documents are gone through, every wavefront with counts of its own)
+    static __device__ __forceinline__ bool fits(const RowRules &r)
+    {
+        return r.n_words <= kSlots / 4 * 3;
+    }
+
+    static __device__ __forceinline__ int slot(int32_t w)
+    {
+        return (int)((uint32_t)w * 0x9E3779B1u >> (32 - kLogSlots));
+    }
+
+    // The workgroup makes it; a barrier has to follow.
+    __device__ __forceinline__ void make(const RowRules &r)
+    {
+        if (!fits(r)) return;
+        for (int i = threadIdx.x; i < kSlots; i += blockDim.x) {
+            word[i] = -1;
+            count[i] = 0;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < (int)r.n_words; i += blockDim.x) {
+            const int32_t w = r.words[i];
+            if (w < 0) continue;
+            int at = slot(w);
+            for (;; at = (at + 1) % kSlots) {
+                const int32_t was = atomicCAS(&word[at], -1, w);
+                if (was == -1 || was == w) break;
+            }
+            atomicAdd(&count[at], 1);
+        }
+    }
+
+    // For the lane's word, where each row of 16 lanes has 16 words from base on.  All lanes
+    // call it.
+    __device__ __forceinline__ int of(const RowRules &r, int32_t base)
+    {
+        const int lane = threadIdx.x & 63;
+        if (fits(r)) {
+            const int32_t w = (int32_t)((uint32_t)base + (lane & 15));
+            int at = slot(w);
+            while (word[at] != w && word[at] != -1) at = (at + 1) % kSlots;
+            return word[at] == w ? count[at] : 0;
+        }
+        int32_t *own = count + (threadIdx.x & ~63u);
+        own[lane] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        constexpr int kEach = 4;
+        for (int64_t i = 0; i < r.n_words; i += 64 * kEach) {
+            int32_t entry[kEach];
 #pragma unroll
-    for (int i = 0; i < kListed; ++i)
-        listed[i] = i * 64 + lane < r.n_words ? r.words[i * 64 + lane] : -1;
-    Law law = law_of(part, chunks, scale, powers);
-    const double log_total = law.is ? log(law.total) : 0.0;
-    for (int32_t t0 = 0; t0 < count; t0 += 64) {
-        const int64_t d = d0 + t0 + lane;
-        const bool here = t0 + lane < count;
-        int32_t my_word = -1;
-        float my_logp = __builtin_nanf("");
-        if (law.is) {
-            const double uniform =
-                !here ? 0.0
-                : u   ? u[d]
-                      : (double)philox_x0(seed, (uint64_t)(draw0 + d), step, kPurposeWord) * 0x1p-32;
-            // (NaN, and 1 or more: the last word with weight)
-            const double my_goal = uniform * law.total < law.total
-                                       ? fmax(uniform * law.total, 0.0)
-                                       : __builtin_inf();
-            const int32_t many = count - t0 < 64 ? count - t0 : 64;
-            for (int32_t t = 0; t < many; ++t) {
-                double goal = of_lane(my_goal, t);
-                int32_t c0 = 0;
-                if (chunks > 64) {
-                    // 64 chunks at a time: the first whose sum exceeds what is left
-                    for (;; c0 += 64) {
-                        lane_chunk(law, part, c0 + lane, chunks, scale, powers);
-                        const double sum = of_lane(law.upto, 63);
-                        if (sum > goal || c0 >= law.last) break;
-                        goal -= sum;
-                    }
-                }
-                // (an infinite goal: the last word with weight, however little it adds)
-                const bool end = !(goal < __builtin_inf());
-                const int at = end ? 63 - __builtin_clzll(__ballot(law.some))
-                                   : choose(law.upto, goal);
-                const double own = of_lane(law.own, at);
-                int b = kBlocks - 1;
-                if (!end) {
-                    if (at) goal -= of_lane(law.upto, at - 1);
-                    goal = goal > 0.0 ? goal * of_lane(law.inverse, at) : 0.0;
-                    const double2 upto = reinterpret_cast<const double2 *>(
-                        blocks + (int64_t)(c0 + at) * kBlocks)[lane];
-                    const int pair = choose(upto.y, goal);
-                    const double mid = of_lane(upto.x, pair), last = of_lane(upto.y, pair);
-                    const bool second = last > goal ? !(mid > goal) : mid < last;
-                    const double before = second ? mid : pair ? of_lane(upto.y, pair - 1) : 0.0;
-                    goal = fmax(goal - before, 0.0);
-                    b = 2 * pair + second;
-                }
-                int64_t b0;
-                float s;
-                double weight;
-                u64 positive;
-                for (;; --b) {
-                    // the block's words, one a lane: everything that is read of them at once
-                    b0 = (int64_t)(c0 + at) * kDrawChunk + b * kBlockWords;
-                    const int64_t w = b0 + lane;
-                    float bias = 0.f;
-                    uint32_t allowed = 0;
-                    s = 0.f;
-                    if (w < V) {
-                        s = (float)x[w];
-                        if (r.bias) bias = r.bias[w];
-                        allowed = r.mask ? r.mask[w >> 5] >> (w & 31) : 1;
-                    }
-                    int32_t n = 0;
-                    auto tally = [&](int32_t entry) {
-                        const uint32_t a = (uint32_t)entry - (uint32_t)b0;
-                        u64 hits = __ballot(a < (uint32_t)kBlockWords && entry >= 0);
-                        while (hits) {
-                            n += __builtin_amdgcn_readlane((int)a, __builtin_ctzll(hits)) == lane;
-                            hits &= hits - 1;
-                        }
-                    };
+            for (int e = 0; e < kEach; ++e)
+                entry[e] = i + 64 * e + lane < r.n_words ? r.words[i + 64 * e + lane] : -1;
 #pragma unroll
-                    for (int i = 0; i < kListed; ++i)
-                        if (i * 64 < r.n_words) tally(listed[i]);
-                    for (int64_t i = kListed * 64; i < r.n_words; i += 64)
-                        tally(i + lane < r.n_words ? r.words[i + lane] : -1);
-                    if (n > 0) s = penalised(r, s, n);
-                    if (r.bias) s = s + bias;
-                    s = allowed & 1u ? s : -__builtin_inff();
-                    weight = weight_of(s, own, scale, powers);
-                    positive = __ballot(weight > 0.0);
-                    // (a chunk's largest score has weight 1, so the search ends)
-                    if (positive || b == 0) break;
-                }
-                const double sums = prefix(weight);
-                const u64 past = __ballot(sums > goal) & positive;
-                const int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(positive | 1);
-                const int32_t got = (int32_t)(b0 + l);
-                const float score =
-                    __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s), l));
-                if (lane == t) {
-                    my_word = got;
-                    my_logp = score;
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t from = (uint32_t)__builtin_amdgcn_readlane(base, 16 * j);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const uint32_t a = (uint32_t)entry[e] - from;
+                    if (a < (uint32_t)kQuarterWords && entry[e] >= 0) atomicAdd(&own[16 * j + a], 1);
                 }
             }
-            my_logp = (float)(((double)my_logp - law.top) * scale *
-                                  (0.693147180559945309417 / 32.0) -
-                              log_total);
         }
-        if (here) {
-            word[d] = my_word;
-            logp[d] = my_logp;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        return own[lane];
+    }
+};
+
+// `count` draws from d0 on of a row by one wavefront.  times(base) is how often a lane's word
+// is listed, where rows of 16 lanes have 16 words each from base on.
+template <typename T, typename F>
+__device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, const RowRules &r,
+                                           double scale, int32_t chunks, const Part *part,
+                                           const double *sums, const Powers &powers, int64_t d0,
+                                           int32_t count, const double *__restrict__ u,
+                                           uint64_t seed, uint32_t step, int64_t draw0,
+                                           int32_t *__restrict__ word, float *__restrict__ logp,
+                                           F times)
+{
+    const int lane = threadIdx.x & 63;
+    double given = u && lane < count ? u[d0 + lane] : 0.0;
+    Law law = law_of(part, chunks, scale, powers);
+    if (!law.is) {
+        for (int32_t t = lane; t < count; t += 64) {
+            word[d0 + t] = -1;
+            logp[d0 + t] = __builtin_nanf("");
+        }
+        return;
+    }
+    const double log_total = log(law.total);
+    for (int32_t t0 = 0; t0 < count; t0 += 64) {
+        const int64_t d = d0 + t0 + lane;
+        const int32_t many = count - t0 < 64 ? count - t0 : 64;
+        if (u && t0 && lane < many) given = u[d];
+        const double uniform =
+            lane >= many ? 0.0
+            : u          ? given
+                         : (double)philox_x0(seed, (uint64_t)(draw0 + d), step, kPurposeWord) * 0x1p-32;
+        // (NaN, and 1 or more: the last word with weight, however little it adds)
+        const bool end = !(uniform * law.total < law.total);
+        double goal = end ? 0.0 : fmax(uniform * law.total, 0.0);
+        // the chunk: 64 at a time, the first whose sum exceeds what is left
+        int32_t chunk = 0;
+        double own = 0.0;
+        bool found = false;
+        for (int32_t c0 = 0;; c0 += 64) {
+            if (chunks > 64) lane_chunk(law, part, c0 + lane, chunks, scale, powers);
+            const double sum = of_lane(law.upto, 63);
+            const bool last = c0 >= law.last;
+            const u64 some = __ballot(law.some);
+            const int at = chunks == 1 ? 0
+                           : end       ? 63 - __builtin_clzll(some | 1)
+                                       : first_past(law.upto, sum, goal);
+            const double before = __shfl(law.upto, at ? at - 1 : 0);
+            const double its = __shfl(law.own, at), inverse = __shfl(law.inverse, at);
+            if (!found && (last || (!end && sum > goal))) {
+                found = true;
+                chunk = min(c0 + at, chunks - 1);
+                own = its;
+                goal = at ? goal - before : goal;
+                goal = goal > 0.0 ? goal * inverse : 0.0;
+            } else if (!found) {
+                goal -= sum;
+            }
+            if (last || !__any(!found)) break;
+        }
+        // the block (four draws' sums requested at a time)
+        int32_t block = 0;
+        for (int32_t t4 = 0; t4 < many; t4 += 4) {
+            double2 upto[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                upto[j] = reinterpret_cast<const double2 *>(
+                    sums + (int64_t)__builtin_amdgcn_readlane(chunk, t4 + j) * kSums)[lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const double g = of_lane(goal, t4 + j);
+                int b = __builtin_popcountll(__ballot(!(upto[j].x > g))) +
+                        __builtin_popcountll(__ballot(!(upto[j].y > g)));
+                if (b == kBlocks) {  // (rounding: the first that reaches the last)
+                    const double end_sum = of_lane(upto[j].y, 63);
+                    b = __builtin_popcountll(__ballot(upto[j].x < end_sum)) +
+                        __builtin_popcountll(__ballot(upto[j].y < end_sum));
+                }
+                const double before =
+                    b ? of_lane(b & 1 ? upto[j].x : upto[j].y, (b - 1) >> 1) : 0.0;
+                if (lane == t4 + j) {
+                    block = b;
+                    goal = fmax(g - before, 0.0);
+                }
+            }
+        }
+        // the quarter
+        const double *of_quarter = sums + (int64_t)chunk * kSums + kBlocks;
+        int32_t quarter = kQuarters - 1;
+        if (end) {
+            while (quarter > 0 && !(of_quarter[quarter] > 0.0)) --quarter;
+            goal = __builtin_inf();
+        } else {
+            const double2 a = reinterpret_cast<const double2 *>(of_quarter)[2 * block];
+            const double2 b = reinterpret_cast<const double2 *>(of_quarter)[2 * block + 1];
+            const double s1 = a.x + a.y, s2 = s1 + b.x, s3 = s2 + b.y;
+            const int q = a.x > goal   ? 0
+                          : s1 > goal  ? 1
+                          : s2 > goal  ? 2
+                          : s3 > goal  ? 3
+                          : b.y > 0.0  ? 3  // (rounding: the last with weight)
+                          : b.x > 0.0  ? 2
+                          : a.y > 0.0  ? 1
+                                       : 0;
+            goal = fmax(goal - (q == 0 ? 0.0 : q == 1 ? a.x : q == 2 ? s1 : s2), 0.0);
+            quarter = 4 * block + q;
+        }
+        const int32_t first = chunk * kDrawChunk + quarter * kQuarterWords;
+        // the word: 16 lanes for a draw, four draws at a time, the scores of 16 requested
+        const int place = lane & 15, group = lane >> 4;
+        for (int32_t t16 = 0; t16 < many; t16 += 16) {
+            int32_t base[4];
+            float score[4], bias[4];
+            uint32_t allowed[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                base[j] = __shfl(first, t16 + 4 * j + group);
+                const int64_t w = (int64_t)base[j] + place;
+                score[j] = bias[j] = 0.f;
+                allowed[j] = 0;
+                if (w < V && t16 + 4 * j < many) {
+                    score[j] = (float)x[w];
+                    if (r.bias) bias[j] = r.bias[w];
+                    allowed[j] = r.mask ? r.mask[w >> 5] >> (w & 31) : 1;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t t = t16 + 4 * j + group;
+                if (t16 + 4 * j >= many) break;
+                const double g = __shfl(goal, t), top = __shfl(own, t);
+                float s = score[j];
+                if (r.n_words > 0) {
+                    const int n = times(base[j]);
+                    if (n > 0) s = penalised(r, s, n);
+                }
+                if (r.bias) s = s + bias[j];
+                s = allowed[j] & 1u ? s : -__builtin_inff();
+                const double weight = weight_of(s, top, scale, powers);
+                const double upto = row_prefix(weight);
+                const u64 positive = __ballot(weight > 0.0), past = __ballot(upto > g) & positive;
+                const uint32_t in_row = (uint32_t)(past >> (lane & 48)) & 0xFFFFu;
+                const uint32_t have = (uint32_t)(positive >> (lane & 48)) & 0xFFFFu;
+                const int l = in_row ? __builtin_ctz(in_row) : 31 - __builtin_clz(have | 1u);
+                if (place == l && t < many) {
+                    word[d0 + t0 + t] = base[j] + place;
+                    logp[d0 + t0 + t] = (float)(((double)s - law.top) * scale *
+                                                    (0.693147180559945309417 / 32.0) -
+                                                log_total);
+                }
+            }
         }
     }
 }
 
-// One workgroup per (row, chunk): its largest score and its sums.  Rows of one chunk are
+// One workgroup per (row, chunk): its largest score and its sums.  Rows of one chunk (ONE) are
 // drawn from at once.
-template <typename T>
-__global__ void __launch_bounds__(kDrawThreads, 8) k_draw_parts(
+template <typename T, bool ONE>
+__global__ void __launch_bounds__(kDrawThreads, ONE ? 4 : 8) k_draw_parts(
     const T *__restrict__ x, int64_t ld, int64_t V, int32_t chunks, spdp_rules rules, double scale,
-    Part *__restrict__ part, double *__restrict__ blocks, int32_t draws,
+    Part *__restrict__ part, double *__restrict__ sums, int32_t draws,
     const double *__restrict__ u, uint64_t seed, uint32_t step, int64_t draw0,
     int32_t *__restrict__ word, float *__restrict__ logp)
 {
     using C = Chunk<T, kDrawThreads, kDrawPer>;
     constexpr int kLanes = kBlockWords / C::N;  // lanes whose vectors make a block
+    constexpr int kQuarterLanes = kQuarterWords / C::N;
     __shared__ typename C::Listed listed;
     __shared__ float wave_top[kDrawThreads / 64];
-    __shared__ alignas(16) double sum_of[kBlocks];
+    __shared__ alignas(16) double sum_of[kSums];
     __shared__ Part own;
     __shared__ Powers powers;
     make_powers(powers);
@@ -835,6 +960,7 @@ __global__ void __launch_bounds__(kDrawThreads, 8) k_draw_parts(
     law = !__syncthreads_or(!law);
     for (int i = 0; i < kDrawThreads / 64; ++i) top = fmaxf(top, wave_top[i]);
     const bool some = top > -__builtin_inff() && top < __builtin_inff();
+    double *to = ONE ? sum_of : sums + (int64_t)blockIdx.x * kSums;
 #pragma unroll
     for (int k = 0; k < C::U; ++k) {
         double s = 0.0;
@@ -842,9 +968,10 @@ __global__ void __launch_bounds__(kDrawThreads, 8) k_draw_parts(
 #pragma unroll
             for (int i = 0; i < C::N; ++i) s += weight_of(v[k][i], top, scale, powers);
         }
-        s = group_sum<kLanes>(s);
-        const int b = C::at(k) / kBlockWords;
-        if (lane % kLanes == 0) sum_of[b] = s;
+        s = quarter_sum<kQuarterLanes>(s);
+        if (lane % kQuarterLanes == 0) to[kBlocks + C::at(k) / kQuarterWords] = s;
+        s = block_sum<kLanes>(s);
+        if (lane % kLanes == 0) sum_of[C::at(k) / kBlockWords] = s;
     }
     __syncthreads();
     if (wave == 0) {
@@ -852,21 +979,22 @@ __global__ void __launch_bounds__(kDrawThreads, 8) k_draw_parts(
         double upto[2];
         rising(share, upto);
         const Part p{law ? (double)top : __builtin_nan(""), of_lane(upto[1], 63)};
-        double *to = chunks > 1 ? blocks + (int64_t)blockIdx.x * kBlocks : sum_of;
         to[2 * lane] = upto[0];
         to[2 * lane + 1] = upto[1];
         if (lane == 0) {
             own = p;
-            if (chunks > 1) part[blockIdx.x] = p;
+            if (!ONE) part[blockIdx.x] = p;
         }
     }
-    if (chunks > 1) return;
-    __syncthreads();
-    constexpr int kWaves = kDrawThreads / 64;
-    const int32_t each = (draws + kWaves - 1) / kWaves, t0 = wave * each;
-    if (t0 < draws)
-        draw_words(x + row * ld, V, r, scale, 1, &own, sum_of, powers, row * draws + t0,
-                   draws - t0 < each ? draws - t0 : each, u, seed, step, draw0, word, logp);
+    if constexpr (ONE) {
+        __syncthreads();
+        constexpr int kWaves = kDrawThreads / 64;
+        const int32_t each = (draws + kWaves - 1) / kWaves, t0 = wave * each;
+        if (t0 < draws)
+            draw_words(x + row * ld, V, r, scale, 1, &own, sum_of, powers, row * draws + t0,
+                       draws - t0 < each ? draws - t0 : each, u, seed, step, draw0, word, logp,
+                       [&](int32_t base) { return listed.count[base + (lane & 15)]; });
+    }
 }
 
 // `share` workgroups of four wavefronts per row, `each` draws a wavefront.
@@ -874,7 +1002,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_draw(const T *__restrict__ x, int64_t ld, int64_t V,
                                               int32_t chunks, spdp_rules rules, double scale,
                                               const Part *__restrict__ part,
-                                              const double *__restrict__ blocks, int32_t share,
+                                              const double *__restrict__ sums, int32_t share,
                                               int32_t each, int32_t draws,
                                               const double *__restrict__ u, uint64_t seed,
                                               uint32_t step, int64_t draw0,
@@ -882,15 +1010,18 @@ __global__ void __launch_bounds__(256) k_draw(const T *__restrict__ x, int64_t l
                                               float *__restrict__ logp)
 {
     __shared__ Powers powers;
+    __shared__ Times times;
     make_powers(powers);
-    __syncthreads();
     const int64_t row = blockIdx.x / (uint32_t)share;
+    const RowRules r = row_rules(rules, row);
+    if (r.n_words > 0) times.make(r);
+    __syncthreads();
     const int64_t t0 = ((int64_t)(blockIdx.x % (uint32_t)share) * 4 + (threadIdx.x >> 6)) * each;
     if (t0 >= draws) return;
-    const RowRules r = row_rules(rules, row);
     draw_words(x + row * ld, V, r, scale, chunks, part + row * chunks,
-               blocks + row * chunks * kBlocks, powers, row * draws + t0,
-               (int32_t)(draws - t0 < each ? draws - t0 : each), u, seed, step, draw0, word, logp);
+               sums + row * chunks * kSums, powers, row * draws + t0,
+               (int32_t)(draws - t0 < each ? draws - t0 : each), u, seed, step, draw0, word, logp,
+               [&](int32_t base) { return times.of(r, base); });
 }
 
 // launch(value of the scores' type, grid), and its error
@@ -929,7 +1060,7 @@ TopShape top_shape(int64_t rows, int64_t V)
 
 int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int64_t kDrawWaves = 16384;
+constexpr int64_t kDrawWaves = 8192;
 
 int64_t draw_parts_bytes(int64_t rows, int64_t chunks)
 {
@@ -961,7 +1092,7 @@ int64_t words_work(int64_t rows, int64_t V, int32_t take)
     const int64_t parts = most < rows + kTopBlocks ? most : rows + kTopBlocks;
     const int64_t chunks = chunks_of(V, kDrawChunk);
     const int64_t top = parts * take * (int64_t)sizeof(u64);
-    const int64_t draw = chunks > 1 ? draw_parts_bytes(rows, chunks) + rows * chunks * kBlocks * 8 : 0;
+    const int64_t draw = chunks > 1 ? draw_parts_bytes(rows, chunks) + rows * chunks * kSums * 8 : 0;
     return round256(top > draw ? top : draw > 0 ? draw : 1);
 }
 
@@ -994,12 +1125,13 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
     const int64_t chunks = chunks_of(V, kDrawChunk);
     const double scale = 32.0 * 1.44269504088896340736 / temperature;
     Part *part = static_cast<Part *>(work);
-    double *blocks = reinterpret_cast<double *>(static_cast<char *>(work) +
-                                                draw_parts_bytes(rows, chunks));
+    double *sums = reinterpret_cast<double *>(static_cast<char *>(work) +
+                                              draw_parts_bytes(rows, chunks));
     hipError_t e = by_type(type, rows * chunks, [&](auto t, dim3 grid) {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_draw_parts<T>, grid, dim3(kDrawThreads), 0, st, (const T *)x, ld, V,
-                           (int32_t)chunks, rules, scale, part, blocks, draws, u, seed, step, draw0,
+        const auto kernel = chunks == 1 ? k_draw_parts<T, true> : k_draw_parts<T, false>;
+        hipLaunchKernelGGL(kernel, grid, dim3(kDrawThreads), 0, st, (const T *)x, ld, V,
+                           (int32_t)chunks, rules, scale, part, sums, draws, u, seed, step, draw0,
                            word, logp);
     });
     if (e != hipSuccess || chunks == 1) return e;
@@ -1011,7 +1143,7 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
     return by_type(type, rows * share, [&](auto t, dim3 grid) {
         using T = decltype(t);
         hipLaunchKernelGGL(k_draw<T>, grid, dim3(256), 0, st, (const T *)x, ld, V, (int32_t)chunks,
-                           rules, scale, part, blocks, (int32_t)share, (int32_t)each, draws, u,
+                           rules, scale, part, sums, (int32_t)share, (int32_t)each, draws, u,
                            seed, step, draw0, word, logp);
     });
 }

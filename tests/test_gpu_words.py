@@ -492,6 +492,57 @@ def test_draw_special_rows(state, V):
     assert (got[8] % 2 == 1).all()
 
 
+@pytest.mark.parametrize("V", [5000, 9000])
+@pytest.mark.parametrize("lens", [(1535, 1536, 1537, 0), (1, 20000, 4096, 1540)])
+def test_draw_from_long_documents(state, V, lens):
+    """Documents around and beyond the length that a table of their words holds, with one word
+    in half of a document's places and penalties that a wrong count would show."""
+    say(f"draw: documents of {lens} words of {V}")
+    rng = np.random.default_rng(V + lens[0])
+    rows, n = len(lens), 200
+    docs = [rng.integers(-3, V + 3, size=m) for m in lens]
+    for i, d in enumerate(docs):
+        d[: len(d) // 2] = V - 1 - i
+    pen = np.stack([1 + rng.random(rows), rng.random(rows), 2.0 ** -9 * rng.random(rows)], 1)
+    pen = pen.astype(np.float32)
+    x = _scores(rng, rows, V, torch.float32)
+    for i in range(rows):
+        x[i, V - 20:] += 6  # (the counted word and its neighbours are drawn often)
+    u = rng.random((rows, n))
+    r = sp.Rules(rows, V, doc_off=dev(np.cumsum([0] + list(lens))),
+                 words=dev(np.concatenate(docs).astype(np.int32)), penalties=dev(pen))
+    word = torch.empty((rows, n), dtype=torch.int32, device="cuda")
+    logp = torch.empty((rows, n), device="cuda")
+    sp.spdp_draw(state.h, x, word, logp, work_for(rows, V), u=dev(u), rules=r)
+    _check_draws(word.cpu().numpy(), logp.cpu().numpy(),
+                 ow.adjusted(x.cpu().numpy(), docs, pen), u, 1.0)
+
+
+def test_draw_of_many_chunks(state):
+    """More chunks than a wavefront has lanes, some of them without weight, the last among
+    them, and more draws than it makes at a time."""
+    say("draw: 1 200 000 words")
+    rng = np.random.default_rng(12)
+    rows, V, n = 3, 1200000, 150
+    x = _scores(rng, rows, V, torch.float32)
+    x[0, 700000:] = -np.inf
+    x[1, : 600000] = -np.inf
+    x[2, 8192 * 64: 8192 * 128] = -np.inf
+    u = rng.random((rows, n))
+    u[:, 0] = 0.0
+    u[:, 77] = 1.0
+    u[:, 149] = np.nan
+    word = torch.empty((rows, n), dtype=torch.int32, device="cuda")
+    logp = torch.empty((rows, n), device="cuda")
+    sp.spdp_draw(state.h, x, word, logp, work_for(rows, V), u=dev(u))
+    word, logp = word.cpu().numpy(), logp.cpu().numpy()
+    ends = [699999, V - 1, V - 1]
+    np.testing.assert_array_equal(word[:, 77], ends)
+    np.testing.assert_array_equal(word[:, 149], ends)
+    keep = [i for i in range(n) if i not in (77, 149)]
+    _check_draws(word[:, keep], logp[:, keep], x.cpu().numpy(), u[:, keep], 1.0)
+
+
 def test_draw_by_seed(state):
     say("draw by seed")
     rng = np.random.default_rng(8)
