@@ -22,12 +22,15 @@ __global__ void __launch_bounds__(kAdjustThreads) k_adjust(const T *x, int64_t l
     C c;
     c.request(x + row * ldx, w0, V);
     const RowRules r = row_rules(rules, row);
+    typename C::Held held[C::U];
+#pragma unroll
+    for (int u = 0; u < C::U; ++u) C::hold(r, w0, V, u, held[u]);
     if (r.n_words > 0) C::count(r, w0, listed);
     T *out = y + row * ldy + w0;
 #pragma unroll
     for (int u = 0; u < C::U; ++u) {
         float v[C::N];
-        c.scores(r, w0, V, listed, u, v);
+        c.scores(r, w0, V, listed, u, v, &held[u]);
         Vec<T> k;
 #pragma unroll
         for (int i = 0; i < C::N; ++i) k.v[i] = (T)v[i];
@@ -339,7 +342,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
 #pragma unroll
             for (int i = 0; i < C::N; ++i) pass += v[u][i] >= low;
         int passing, to = places(pass, n, wave_pass[chunk & 1], passing);
-        if (n + passing <= kKeys) {
+        if (__builtin_expect(n + passing <= kKeys, 1)) {
             if (pass) {
 #pragma unroll
                 for (int u = 0; u < C::U; ++u)
@@ -352,30 +355,35 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
             if (r.n_words > 0) __syncthreads();  // (before the next chunk's words are counted)
             continue;
         }
-        // (kKeys / 2 scores at a time, so that there is room after every cut)
+        // kKeys / 2 scores at a time, so that there is room after every cut, from LDS (the
+        // counts are not needed any more)
+        float *score = reinterpret_cast<float *>(listed.count);
 #pragma unroll
         for (int u = 0; u < C::U; ++u)
 #pragma unroll
-            for (int i = 0; i < C::N; i += 4) {
-                __syncthreads();
-                if (n > kKeys / 2) {
-                    u64 least;
-                    n = cut_keys(kept, n, k, least);
-                    bound = least > bound ? least : bound;
-                }
-                u64 key[4];
-                int more = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    key[e] = key_of(v[u][i + e], w0 + C::at(u) + i + e);
-                    more += key[e] >= bound;
-                }
-                int at = places(more, n, wave_pass[0], passing);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (key[e] >= bound) kept.key[at++] = key[e];
-                n += passing;
+            for (int i = 0; i < C::N; ++i) score[C::at(u) + i] = v[u][i];
+        constexpr int kEach = kKeys / 2 / kTopThreads;
+        for (int from = 0; from < C::kWords; from += kEach * kTopThreads) {
+            __syncthreads();
+            if (n > kKeys / 2) {
+                u64 least;
+                n = cut_keys(kept, n, k, least);
+                bound = least > bound ? least : bound;
             }
+            u64 key[kEach];
+            int more = 0;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int at = from + e * kTopThreads + threadIdx.x;
+                key[e] = key_of(score[at], w0 + at);
+                more += key[e] >= bound;
+            }
+            int at = places(more, n, wave_pass[0], passing);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e)
+                if (key[e] >= bound) kept.key[at++] = key[e];
+            n += passing;
+        }
         __syncthreads();
     }
     __syncthreads();
@@ -942,13 +950,16 @@ __global__ void __launch_bounds__(kDrawThreads, ONE ? 4 : 8) k_draw_parts(
     C c;
     c.request(x + row * ld, w0, V);
     const RowRules r = row_rules(rules, row);
+    typename C::Held held[C::U];
+#pragma unroll
+    for (int u = 0; u < C::U; ++u) C::hold(r, w0, V, u, held[u]);
     if (r.n_words > 0) C::count(r, w0, listed);
     float v[C::U][C::N];
     float top = -__builtin_inff();
     bool law = true;
 #pragma unroll
     for (int k = 0; k < C::U; ++k) {
-        c.scores(r, w0, V, listed, k, v[k]);
+        c.scores(r, w0, V, listed, k, v[k], &held[k]);
 #pragma unroll
         for (int i = 0; i < C::N; ++i) {
             law = law && v[k][i] < __builtin_inff();

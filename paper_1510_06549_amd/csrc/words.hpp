@@ -11,10 +11,9 @@
 // The steps are rounded one by one (no fused multiply-add), so that the kernels
 // that store the result and those that choose from it see the same scores.
 //
-// A row is taken in chunks by workgroups, 16 bytes of scores a load.  Few words of a
-// chunk are listed: a bitmap in LDS says which, and only for those is a count kept,
-// cleared and added up (integer atomics, so their order does not matter) by walking
-// the document's words twice.
+// A row is taken in chunks by workgroups, 16 bytes of scores a load.  Counts of a chunk's
+// words are added up in LDS by walking the document's words (integer atomics, so their
+// order does not matter); few words of a chunk are listed, and a bitmap says which.
 #pragma once
 
 #include "spdp_internal.hpp"
@@ -166,9 +165,36 @@ struct Chunk {
         __syncthreads();
     }
 
-    // The scores of vector u under the rules; -inf past the row's end.
+    // What the row's bias and mask hold for a vector of scores.
+    struct Held {
+        float bias[N];
+        uint32_t allowed;
+    };
+
+    // Request them for vector u, to be under way while the listed words are counted.
+    static __device__ __forceinline__ void hold(const RowRules &r, int64_t w0, int64_t V, int u,
+                                                Held &h)
+    {
+        const int64_t w = w0 + at(u);
+        if (w + N > V) return;  // (the scores at a row's end look up their own)
+        if (r.bias) {
+            typedef float quad __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                const quad b = *reinterpret_cast<const quad *>(r.bias + w + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) h.bias[i + k] = b[k];
+            }
+        }
+        // (w is a multiple of N, so its bits lie in one byte)
+        if (r.mask) h.allowed = reinterpret_cast<const uint8_t *>(r.mask)[w >> 3];
+    }
+
+    // The scores of vector u under the rules; -inf past the row's end.  Without `held` (for
+    // kernels that have no registers to hold them) bias and mask are read here.
     __device__ __forceinline__ void scores(const RowRules &r, int64_t w0, int64_t V,
-                                           const Listed &l, int u, float (&x)[N]) const
+                                           const Listed &l, int u, float (&x)[N],
+                                           const Held *held = nullptr) const
     {
         const int a = at(u);
         const int64_t w = w0 + a;
@@ -191,18 +217,15 @@ struct Chunk {
                     if (seen >> i & 1u) x[i] = penalised(r, x[i], l.count[a + i]);
             }
         }
+        Held own;
+        if (!held) hold(r, w0, V, u, own);
+        const Held &h = held ? *held : own;
         if (r.bias) {
-            typedef float quad __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-            for (int i = 0; i < N; i += 4) {
-                const quad b = *reinterpret_cast<const quad *>(r.bias + w + i);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[i + k] = x[i + k] + b[k];
-            }
+            for (int i = 0; i < N; ++i) x[i] = x[i] + h.bias[i];
         }
         if (r.mask) {
-            // (w is a multiple of N, so its bits lie in one byte)
-            const uint32_t ok = reinterpret_cast<const uint8_t *>(r.mask)[w >> 3] >> (w & 7);
+            const uint32_t ok = h.allowed >> (w & 7);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = ok >> i & 1u ? x[i] : -__builtin_inff();
         }
