@@ -1051,7 +1051,9 @@ int64_t chunks_of(int64_t V, int64_t words) { return (V + words - 1) / words; }
 // Parts of a row for the best words, of even length: as many as chunks while the rows alone
 // leave compute units idle, else several chunks one after another in a workgroup (few
 // scores of the later ones pass the bound), all parts of all rows at once on the chip
-// (four workgroups a compute unit; 400 rows of 50 000: two parts 58 us, three 71, four 66).
+// (four workgroups a compute unit; 400 rows of 50 000 without rules: two parts 33 us, one 35,
+// four 41).  Two chunks are taken by one workgroup, which is sooner done than the parts are
+// joined (1 row of 8 192 words 7.6 us, in two parts 10.1; 12 288 words 13.0, in three 10.7).
 constexpr int64_t kTopBlocks = 1024;
 
 struct TopShape {
@@ -1062,7 +1064,7 @@ TopShape top_shape(int64_t rows, int64_t V)
 {
     const int64_t chunks = chunks_of(V, kTopThreads * 16);
     int64_t parts = rows > 0 && rows < kTopBlocks ? kTopBlocks / rows : 1;
-    parts = parts > chunks ? chunks : parts;
+    parts = chunks <= 2 ? 1 : parts > chunks ? chunks : parts;
     const int64_t per = (chunks + parts - 1) / parts;  // chunks of a part
     parts = (chunks + per - 1) / per;
     const int64_t words = ((V + parts - 1) / parts + 31) / 32 * 32;  // (masks' words)
