@@ -356,13 +356,12 @@ int spdp_pack8(spdp_state *s, const void *x, int32_t type, int64_t ld, const spd
 /*
  * c[i][j] = sum_k a[i][k] b[j][k] of rows in 8 bits with the same columns, the
  * elements exact (bf16, which holds them for scales of 2^-124 to 2^119; beyond, they
- * round to bf16 or become infinite) and sums in fp32, or its natural logarithm if log_scores != 0 (-inf where the sum is 0, NaN
- * where it is negative), rounded to `type` (SPDP_F32, SPDP_F16 or SPDP_BF16).  c is
+ * round to bf16 or become infinite) and sums in fp32, or its natural logarithm if
+ * log_scores != 0 (-inf where the sum is 0, NaN where it is negative), rounded to `type` (SPDP_F32, SPDP_F16 or SPDP_BF16).  c is
  * device [a->rows][b->rows] with ld elements from one row to the next; elements
  * behind a row's end are left as they are.
  * Errors: E_ARG (NULL pointer, sizes out of range or columns that differ, ld <
- * b->rows, another type, buffers as for spdp_pack8), E_RANGE (more than 2^31 tiles
- * of 16 x 16 outputs), E_HIP.
+ * b->rows, another type, buffers as for spdp_pack8), E_HIP.
  */
 int spdp_product8(spdp_state *s, const spdp_rows8 *a, const spdp_rows8 *b, int32_t log_scores,
                   void *c, int32_t type, int64_t ld);
@@ -405,8 +404,7 @@ typedef struct {
  * ldy = ldx; other overlaps, of the memory from the first element to the last, are an
  * error.  Elements behind a row's end are left as they are.
  * Errors: E_ARG (NULL pointer, sizes out of range, rules of another size or
- * incomplete, another type, overlapping buffers, buffers as for spdp_pack8),
- * E_RANGE (more than 2^31 chunks of 4096 scores), E_HIP.
+ * incomplete, another type, overlapping buffers, buffers as for spdp_pack8), E_HIP.
  */
 int spdp_adjust(spdp_state *s, const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
                 const spdp_rules *rules);
@@ -421,7 +419,7 @@ int spdp_words_work(int64_t rows, int32_t n_words, int32_t take, int64_t *bytes)
  * word.  Scores that are -inf or NaN are never taken; places that are left hold
  * word -1 and value -inf.  work: device, 16-byte aligned.
  * Errors: E_ARG (as spdp_adjust; k outside [1, SPDP_MAX_TAKE]; a workspace that is
- * too small or not aligned), E_RANGE, E_HIP.
+ * too small or not aligned), E_HIP.
  */
 int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
              int32_t n_words, const spdp_rules *rules, int32_t k, int32_t *word, float *value,
@@ -438,7 +436,7 @@ int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t row
  * A row without a law (every score -inf; NaN or +inf among them) gives word -1 and
  * logp NaN.
  * Errors: E_ARG (as spdp_top; draws outside [0, 2^20], temperature outside [1e-6, 1e6]),
- * E_RANGE, E_HIP.
+ * E_HIP.
  */
 int spdp_draw(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
               int32_t n_words, const spdp_rules *rules, double temperature, int32_t draws,

@@ -1174,13 +1174,6 @@ int check_rules(const spdp_state *s, const spdp_rules *r, int64_t rows, int64_t 
     return SPDP_OK;
 }
 
-int check_blocks(int64_t blocks)
-{
-    if (blocks > INT32_MAX)
-        return fail(SPDP_E_RANGE, "%lld workgroups exceed a launch", (long long)blocks);
-    return SPDP_OK;
-}
-
 int check_work(const spdp_state *s, const void *work, int64_t have, int64_t need)
 {
     if (have < need)
@@ -1209,19 +1202,6 @@ int check_draws(const spdp_state *s, int32_t draws, double temperature, int64_t 
     return check_device(s, logp, rows * draws * 4, 4, "logp");
 }
 
-// The rules of the rows from `row` on.
-spdp_rules rules_from(const spdp_rules &r, int64_t row)
-{
-    spdp_rules o = r;
-    if (o.doc_off) {
-        o.doc_off += row;
-        o.penalties += 3 * row;
-    }
-    if (o.bias_of) o.bias_of += row;
-    if (o.mask_of) o.mask_of += row;
-    return o;
-}
-
 // Workspace of spdp_predict for `rows` documents at a time: their scores (unless
 // the caller keeps them), then what choosing words needs.
 int64_t scores_room(int64_t rows, int64_t n, int32_t type, bool kept)
@@ -1242,7 +1222,6 @@ int spdp_pack8(spdp_state *s, const void *x, int32_t type, int64_t ld, const spd
     int64_t bytes = 0;
     CALL(matrix_bytes(out->rows, out->cols, ld, type, "x", &bytes));
     CALL(check_device(s, x, bytes, (int)type_size(type), "x"));
-    CALL(check_blocks(out->rows * blocks8(out->cols) / 4 + 1));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_pack8(x, type, out->rows, out->cols, ld, out->q, out->e, s->st));
@@ -1259,7 +1238,6 @@ int spdp_product8(spdp_state *s, const spdp_rows8 *a, const spdp_rows8 *b, int32
         return fail(SPDP_E_ARG, "rows of %d and %d columns", a->cols, b->cols);
     if (b->rows == 0) return SPDP_OK;
     CALL(check_scores(s, c, ld, type, a->rows, b->rows, "c"));
-    CALL(check_blocks((a->rows + 15) / 16 * ((b->rows + 15) / 16)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_product8(*a, *b, log_scores != 0, c, type, ld, s->st));
@@ -1282,7 +1260,6 @@ int spdp_adjust(spdp_state *s, const void *x, int64_t ldx, void *y, int64_t ldy,
         if (x0 < y1 && y0 < x1)
             return fail(SPDP_E_ARG, "x and y overlap and are not the same rows");
     }
-    CALL(check_blocks(words_blocks(rows, n)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_adjust(x, ldx, y, ldy, type, rows, n, *rules, s->st));
@@ -1307,7 +1284,6 @@ int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t row
     if (rules) CALL(check_rules(s, rules, rows, n_words));
     CALL(check_take(s, k, rows, word, value));
     CALL(check_work(s, work, work_bytes, words_work(rows, n_words, k)));
-    CALL(check_blocks(words_blocks(rows, n_words)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_top(x, ld, type, rows, n_words, rules ? *rules : spdp_rules{}, k, word, value,
@@ -1325,7 +1301,6 @@ int spdp_draw(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t ro
     if (rules) CALL(check_rules(s, rules, rows, n_words));
     CALL(check_draws(s, draws, temperature, rows, u, word, logp));
     CALL(check_work(s, work, work_bytes, words_work(rows, n_words, 0)));
-    CALL(check_blocks(words_blocks(rows, n_words)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_draw(x, ld, type, rows, n_words, rules ? *rules : spdp_rules{}, temperature,
@@ -1383,8 +1358,6 @@ int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
         rows = low > kPredictTile ? low - low % kPredictTile : low;
     }
     CALL(check_work(s, work, work_bytes, need(rows)));
-    CALL(check_blocks(words_blocks(rows, V)));
-    CALL(check_blocks((rows + 15) / 16 * ((V + 15) / 16)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     const int64_t blocks = blocks8(docs->cols);

@@ -63,8 +63,8 @@ __device__ __forceinline__ int max32(int v)
 }
 
 // Half a wavefront per (row, block), four columns a lane, UNITS blocks whose columns are all
-// requested first (one of doubles, two of floats: 100 000 rows of 500 take 79 and 58 us); whole numbers throughout, as the scale is an
-// exponent and the rounding bits.
+// requested first (one of doubles, two of floats: 100 000 rows of 500 take 79 and 58 us); whole
+// numbers throughout, as the scale is an exponent and the rounding bits.
 template <typename T, int UNITS>
 __global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, int64_t units,
                                                int32_t cols, int64_t ld, int32_t nb,
@@ -534,24 +534,45 @@ hipError_t launch_pack8(const void *x, int32_t type, int64_t rows, int32_t cols,
 {
     const int32_t nb = blocks8(cols);
     if (rows == 0 || nb == 0) return hipSuccess;
-    const int64_t units = rows * nb;
-    const auto blocks = [&](int per) { return dim3((unsigned)((units + 8 * per - 1) / (8 * per))); };
-    if (type == SPDP_F64)
-        hipLaunchKernelGGL((k_pack8<double, 1>), blocks(1), dim3(256), 0, st, (const double *)x,
-                           units, cols, ld, nb, q, e);
-    else
-        hipLaunchKernelGGL((k_pack8<float, 2>), blocks(2), dim3(256), 0, st, (const float *)x,
-                           units, cols, ld, nb, q, e);
-    return hipGetLastError();
+    const int64_t step = kLaunchBlocks / nb * 8;  // (rows of a launch; nb is at most 2^17)
+    for (int64_t row = 0; row < rows; row += step) {
+        const int64_t units = (rows - row < step ? rows - row : step) * nb;
+        const auto blocks = [&](int per) {
+            return dim3((unsigned)((units + 8 * per - 1) / (8 * per)));
+        };
+        uint8_t *to = q + row * nb * kBlock, *scales = e + row * nb;
+        if (type == SPDP_F64)
+            hipLaunchKernelGGL((k_pack8<double, 1>), blocks(1), dim3(256), 0, st,
+                               (const double *)x + row * ld, units, cols, ld, nb, to, scales);
+        else
+            hipLaunchKernelGGL((k_pack8<float, 2>), blocks(2), dim3(256), 0, st,
+                               (const float *)x + row * ld, units, cols, ld, nb, to, scales);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_product8(const spdp_rows8 &a, const spdp_rows8 &b, bool log, void *c,
                            int32_t type, int64_t ld, hipStream_t st)
 {
-    if (a.rows == 0 || b.rows == 0) return hipSuccess;
-    if (type == SPDP_F32) return product<float>(a, b, log, c, ld, st);
-    if (type == SPDP_F16) return product<_Float16>(a, b, log, c, ld, st);
-    return product<__bf16>(a, b, log, c, ld, st);
+    // (launches hold 2^24 documents and 2^28 words: 2^20 tiles of 16 documents, or 2^22 of 64
+    // words for up to 16 documents)
+    constexpr int64_t kDocs = 1 << 24, kWords = 1 << 28;
+    const int64_t nb = blocks8(a.cols), size = type == SPDP_F32 ? 4 : 2;
+    for (int64_t d = 0; d < a.rows; d += kDocs)
+        for (int64_t w = 0; w < b.rows; w += kWords) {
+            const spdp_rows8 docs{a.rows - d < kDocs ? a.rows - d : kDocs, a.cols,
+                                  a.q + d * nb * kBlock, a.e + d * nb};
+            const spdp_rows8 words{b.rows - w < kWords ? b.rows - w : kWords, b.cols,
+                                   b.q + w * nb * kBlock, b.e + w * nb};
+            void *to = static_cast<char *>(c) + (d * ld + w) * size;
+            const hipError_t e = type == SPDP_F32   ? product<float>(docs, words, log, to, ld, st)
+                                 : type == SPDP_F16 ? product<_Float16>(docs, words, log, to, ld, st)
+                                                    : product<__bf16>(docs, words, log, to, ld, st);
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
 }
 
 }  // namespace spdp

@@ -362,7 +362,22 @@ constexpr int64_t kStreamBytes = 64 << 20;    // scores above it are streamed pa
 // time, 787 with 96, 702 with 400 and 640 with all 800.
 constexpr int64_t kPredictScores = 512 << 20;
 constexpr int64_t kPredictTile = 128;
+// Workgroups of a launch, of up to 512 threads: a launch counts threads in 32 bits.  More rows
+// than that are taken by several launches.
+constexpr int64_t kLaunchBlocks = (1 << 23) - 1;
 inline int32_t blocks8(int32_t cols) { return (cols + kBlock8 - 1) / kBlock8; }
+// the rules of the rows from `row` on
+inline spdp_rules rules_from(const spdp_rules &r, int64_t row)
+{
+    spdp_rules o = r;
+    if (o.doc_off) {
+        o.doc_off += row;
+        o.penalties += 3 * row;
+    }
+    if (o.bias_of) o.bias_of += row;
+    if (o.mask_of) o.mask_of += row;
+    return o;
+}
 hipError_t launch_pack8(const void *x, int32_t type, int64_t rows, int32_t cols, int64_t ld,
                         uint8_t *q, uint8_t *e, hipStream_t st);
 hipError_t launch_product8(const spdp_rows8 &a, const spdp_rows8 &b, bool log, void *c,
@@ -370,7 +385,6 @@ hipError_t launch_product8(const spdp_rows8 &a, const spdp_rows8 &b, bool log, v
 hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
                          int64_t rows, int64_t V, const spdp_rules &rules, hipStream_t st);
 int64_t words_work(int64_t rows, int64_t V, int32_t take);  // bytes for either of the next two
-int64_t words_blocks(int64_t rows, int64_t V);              // workgroups of a launch
 hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
                       const spdp_rules &rules, int32_t k, int32_t *word, float *value, void *work,
                       hipStream_t st);

@@ -1046,6 +1046,20 @@ hipError_t by_type(int32_t type, int64_t blocks, F launch)
     return hipGetLastError();
 }
 
+// launch(first row, rows, their scores) for as many rows at a time as their workgroups fit a
+// launch, per_row at most for one (2^19 at most: 2^31 words in chunks of 4 096).
+template <typename F>
+hipError_t by_rows(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t per_row, F launch)
+{
+    const int64_t step = kLaunchBlocks / per_row, size = type == SPDP_F32 ? 4 : 2;
+    for (int64_t row = 0; row < rows; row += step) {
+        const int64_t m = rows - row < step ? rows - row : step;
+        const hipError_t e = launch(row, m, static_cast<const char *>(x) + row * ld * size);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 int64_t chunks_of(int64_t V, int64_t words) { return (V + words - 1) / words; }
 
 // Parts of a row for the best words, of even length: as many as chunks while the rows alone
@@ -1088,12 +1102,14 @@ hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32
 {
     if (rows == 0 || V == 0) return hipSuccess;
     const int64_t chunks = chunks_of(V, kAdjustThreads * 16);
-    return by_type(type, rows * chunks, [&](auto t, dim3 grid) {
-        using T = decltype(t);
-        const auto kernel = rows * V * (int64_t)sizeof(T) > kStreamBytes ? k_adjust<T, true>
-                                                                         : k_adjust<T, false>;
-        hipLaunchKernelGGL(kernel, grid, dim3(kAdjustThreads), 0, st, (const T *)x, ldx, (T *)y,
-                           ldy, V, (int32_t)chunks, rules);
+    return by_rows(x, ldx, type, rows, chunks, [&](int64_t row, int64_t m, const void *from) {
+        return by_type(type, m * chunks, [&](auto t, dim3 grid) {
+            using T = decltype(t);
+            const auto kernel = rows * V * (int64_t)sizeof(T) > kStreamBytes ? k_adjust<T, true>
+                                                                             : k_adjust<T, false>;
+            hipLaunchKernelGGL(kernel, grid, dim3(kAdjustThreads), 0, st, (const T *)from, ldx,
+                               (T *)y + row * ldy, ldy, V, (int32_t)chunks, rules_from(rules, row));
+        });
     });
 }
 
@@ -1109,24 +1125,26 @@ int64_t words_work(int64_t rows, int64_t V, int32_t take)
     return round256(top > draw ? top : draw > 0 ? draw : 1);
 }
 
-int64_t words_blocks(int64_t rows, int64_t V) { return rows * chunks_of(V, kTopThreads * 16); }
-
 hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
                       const spdp_rules &rules, int32_t k, int32_t *word, float *value, void *work,
                       hipStream_t st)
 {
     if (rows == 0 || k == 0) return hipSuccess;
-    const TopShape s = top_shape(rows, V);
     u64 *best = static_cast<u64 *>(work);
-    hipError_t e = by_type(type, rows * s.parts, [&](auto t, dim3 grid) {
-        using T = decltype(t);
-        hipLaunchKernelGGL(k_top_part<T>, grid, dim3(kTopThreads), 0, st, (const T *)x, ld, V,
-                           (int32_t)s.parts, s.words, rules, k, best, word, value);
+    const int64_t chunks = chunks_of(V, kTopThreads * 16);
+    return by_rows(x, ld, type, rows, chunks, [&](int64_t row, int64_t m, const void *from) {
+        const TopShape s = top_shape(m, V);
+        const hipError_t e = by_type(type, m * s.parts, [&](auto t, dim3 grid) {
+            using T = decltype(t);
+            hipLaunchKernelGGL(k_top_part<T>, grid, dim3(kTopThreads), 0, st, (const T *)from, ld,
+                               V, (int32_t)s.parts, s.words, rules_from(rules, row), k, best,
+                               word + row * k, value + row * k);
+        });
+        if (e != hipSuccess || s.parts == 1) return e;
+        hipLaunchKernelGGL(k_top_join, dim3((unsigned)m), dim3(kTopThreads), 0, st, best,
+                           (int32_t)s.parts, k, word + row * k, value + row * k);
+        return hipGetLastError();
     });
-    if (e != hipSuccess || s.parts == 1) return e;
-    hipLaunchKernelGGL(k_top_join, dim3((unsigned)rows), dim3(kTopThreads), 0, st, best,
-                       (int32_t)s.parts, k, word, value);
-    return hipGetLastError();
 }
 
 hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
@@ -1137,27 +1155,32 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
     if (rows == 0 || draws == 0) return hipSuccess;
     const int64_t chunks = chunks_of(V, kDrawChunk);
     const double scale = 32.0 * 1.44269504088896340736 / temperature;
-    Part *part = static_cast<Part *>(work);
-    double *sums = reinterpret_cast<double *>(static_cast<char *>(work) +
-                                              draw_parts_bytes(rows, chunks));
-    hipError_t e = by_type(type, rows * chunks, [&](auto t, dim3 grid) {
-        using T = decltype(t);
-        const auto kernel = chunks == 1 ? k_draw_parts<T, true> : k_draw_parts<T, false>;
-        hipLaunchKernelGGL(kernel, grid, dim3(kDrawThreads), 0, st, (const T *)x, ld, V,
-                           (int32_t)chunks, rules, scale, part, sums, draws, u, seed, step, draw0,
-                           word, logp);
-    });
-    if (e != hipSuccess || chunks == 1) return e;
-    // a wavefront per draw while that does not fill the chip, then several each
-    int64_t waves = (kDrawWaves + rows - 1) / rows;
-    waves = waves > draws ? draws : waves;
-    const int64_t each = (draws + waves - 1) / waves;
-    const int64_t share = (draws + 4 * each - 1) / (4 * each);
-    return by_type(type, rows * share, [&](auto t, dim3 grid) {
-        using T = decltype(t);
-        hipLaunchKernelGGL(k_draw<T>, grid, dim3(256), 0, st, (const T *)x, ld, V, (int32_t)chunks,
-                           rules, scale, part, sums, (int32_t)share, (int32_t)each, draws, u,
-                           seed, step, draw0, word, logp);
+    return by_rows(x, ld, type, rows, chunks, [&](int64_t row, int64_t m, const void *from) {
+        Part *part = static_cast<Part *>(work);
+        double *sums = reinterpret_cast<double *>(static_cast<char *>(work) +
+                                                  draw_parts_bytes(m, chunks));
+        const spdp_rules r = rules_from(rules, row);
+        const int64_t at = row * draws;
+        const double *given = u ? u + at : nullptr;
+        const hipError_t e = by_type(type, m * chunks, [&](auto t, dim3 grid) {
+            using T = decltype(t);
+            const auto kernel = chunks == 1 ? k_draw_parts<T, true> : k_draw_parts<T, false>;
+            hipLaunchKernelGGL(kernel, grid, dim3(kDrawThreads), 0, st, (const T *)from, ld, V,
+                               (int32_t)chunks, r, scale, part, sums, draws, given, seed, step,
+                               draw0 + at, word + at, logp + at);
+        });
+        if (e != hipSuccess || chunks == 1) return e;
+        // a wavefront per draw while that does not fill the chip, then several each
+        int64_t waves = (kDrawWaves + m - 1) / m;
+        waves = waves > draws ? draws : waves;
+        const int64_t each = (draws + waves - 1) / waves;
+        const int64_t share = (draws + 4 * each - 1) / (4 * each);
+        return by_type(type, m * share, [&](auto t, dim3 grid) {
+            using T = decltype(t);
+            hipLaunchKernelGGL(k_draw<T>, grid, dim3(256), 0, st, (const T *)from, ld, V,
+                               (int32_t)chunks, r, scale, part, sums, (int32_t)share, (int32_t)each,
+                               draws, given, seed, step, draw0 + at, word + at, logp + at);
+        });
     });
 }
 

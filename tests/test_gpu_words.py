@@ -824,3 +824,76 @@ def test_captured_and_on_streams():
             assert torch.equal(a.nan_to_num(5.0), b.nan_to_num(5.0))
     s.close()
     e.close()
+
+
+# ---------------------------------------------------------------------------
+# more rows than a launch holds
+# ---------------------------------------------------------------------------
+LAUNCH = (1 << 23) - 1  # workgroups
+
+
+def test_more_rows_than_a_launch_holds(state):
+    say("adjust, top and draw of 2^23 + 9 rows of 3 words")
+    rng = np.random.default_rng(31)
+    rows, V, seed = LAUNCH + 10, 3, 77
+    x = torch.empty((rows, V), dtype=torch.float16, device="cuda").normal_()
+    bias = torch.tensor([[0.5, -0.25, 1.0], [2.0, 0.0, -1.0]], device="cuda")
+    of = torch.randint(-1, 2, (rows,), dtype=torch.int32, device="cuda")
+    r = sp.Rules(rows, V, bias=bias, bias_of=of)
+    y = sp.spdp_adjust(state.h, x, r, torch.empty_like(x))
+    add = torch.where(of[:, None] >= 0, bias[of.clamp(min=0).long()], torch.zeros((), device="cuda"))
+    assert torch.equal(y, (x.float() + add).half())
+    word = torch.empty((rows, 2), dtype=torch.int32, device="cuda")
+    value = torch.empty((rows, 2), device="cuda")
+    sp.spdp_top(state.h, x, word, value, work_for(rows, V, 2), rules=r)
+    sample = np.r_[0:5, LAUNCH - 5:rows, rng.integers(0, rows, 500)]
+    xs = (x.float() + add)[dev(sample)].cpu().numpy()
+    want = ow.top(xs, 2)
+    np.testing.assert_array_equal(word[dev(sample)].cpu().numpy(), want[0])
+    np.testing.assert_array_equal(value[dev(sample)].cpu().numpy(), want[1])
+    sp.spdp_draw(state.h, x, word, value, work_for(rows, V), rules=r, seed=seed, step=3)
+    u = np.array([[oracle.philox_word0(seed, 2 * i + t, 3, 4) for t in range(2)]
+                  for i in sample.tolist()]) * 2.0 ** -32
+    _check_draws(word[dev(sample)].cpu().numpy(), value[dev(sample)].cpu().numpy(), xs, u, 1.0)
+
+
+def test_more_packed_rows_than_a_launch_holds(state):
+    say("pack of 2^26 rows and products of 2^24 and 2^28")
+    rows = 8 * LAUNCH + 3
+    x = torch.arange(rows, device="cuda", dtype=torch.int32).remainder_(16).float()[:, None]
+    p = sp.spdp_pack8(state.h, x, sp.Rows8.empty(rows, 1))
+    for i in range(0, rows, 1 << 24):
+        q = p.q[i:i + (1 << 24), 0].float() * p.e[i:i + (1 << 24), 0].float().sub_(127).exp2_()
+        assert torch.equal(q, x[i:i + (1 << 24), 0])  # (4 bits: exact)
+    del p, x, q
+    for m, n in (((1 << 24) + 5, 3), (2, (1 << 28) + 70)):
+        sides = []
+        for size in (m, n):
+            q = torch.zeros((size, 128), dtype=torch.uint8, device="cuda")
+            q[:, 0] = 0x38  # 1
+            e = torch.full((size, 1), 127, dtype=torch.uint8, device="cuda")
+            e[-1] = 128
+            e[0] = 129
+            sides.append((sp.Rows8(q.view(torch.float8_e4m3fn), e, 1),
+                          e[:, 0].float().sub_(127).exp2_()))
+        (a, fa), (b, fb) = sides
+        c = torch.empty((m, n), dtype=torch.float16, device="cuda")
+        sp.spdp_product8(state.h, a, b, c)
+        assert torch.equal(c, (fa[:, None] * fb[None, :]).half())
+        del sides, a, b, c, q, e, fa, fb
+
+
+def test_smallest_scores(state):
+    """Scores below the normal range of fp32 keep their order, next to zeros of both signs."""
+    say("top of denormal scores")
+    x = np.zeros((2, 9000), np.float32)
+    x[0] = np.arange(9000) % 4500 * np.float32(1.4e-45)
+    x[1] = -x[0]
+    x[1, ::7] = 0.0
+    for k in (1, 50, 256):
+        word = torch.empty((2, k), dtype=torch.int32, device="cuda")
+        value = torch.empty((2, k), device="cuda")
+        sp.spdp_top(state.h, dev(x), word, value, work_for(2, 9000, k))
+        want = ow.top(x, k)
+        np.testing.assert_array_equal(word.cpu().numpy(), want[0])
+        np.testing.assert_array_equal(value.cpu().numpy(), want[1])
