@@ -360,8 +360,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
                         if (v[u][i] >= low)
                             kept.key[to++] = key_of(v[u][i], w0 + C::at(u) + i);
             }
-            n += passing;
-            if (r.n_words > 0) __syncthreads();  // (before the next chunk's words are counted)
+            n += passing;  // (the counts are free again: all have passed a barrier behind them)
             continue;
         }
         // kKeys / 2 scores at a time, so that there is room after every cut, from LDS (the
