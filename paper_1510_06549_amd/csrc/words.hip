@@ -419,42 +419,54 @@ __global__ void __launch_bounds__(kTopThreads, 4) k_top_part(const T *__restrict
     }
 }
 
-// One workgroup per row: the k best of its parts' keys, k of each part in order.  The last
-// of a run of four keys is reached by all four, so that what (k + 3) / 4 of the threads' runs
-// reach bounds the k best; the keys that reach it are few beside all (k and less than four
-// of each part's, where no thread has more than one run).
+// One workgroup per row: the k best of its parts' keys, k of each part in order.  Where four
+// keys a thread are all, what k of the threads' largest reach bounds the k best.  Of more, the
+// last of a run of four is reached by all four, so that what (k + 3) / 4 of the threads'
+// runs reach does; the keys that reach it are few beside all (k and less than four of each
+// part's, where no thread has more than one run).
 __global__ void __launch_bounds__(kTopThreads) k_top_join(const u64 *__restrict__ best,
                                                           int32_t parts, int32_t k,
                                                           int32_t *__restrict__ word,
                                                           float *__restrict__ value)
 {
+    constexpr int kEach = 4, kAtOnce = kEach * kTopThreads;
+    static_assert(kAtOnce <= kKeys / 2, "room after every cut");
     __shared__ Kept kept;
     __shared__ alignas(16) uint32_t largest[kTopThreads];
     const int64_t row = blockIdx.x;
     const int n = parts * k;
     best += row * n;
-    const int run = k < 4 ? 1 : 4, runs = k / run;  // (of a part; keys behind them are in none)
-    uint32_t mine = 0;
-    for (int i = threadIdx.x; i < parts * runs; i += kTopThreads) {
-        const int part = i / runs;
-        const u64 key = best[part * k + (i - part * runs) * run + run - 1];
-        const uint32_t order = (uint32_t)(key >> 32);
-        mine = mine > order ? mine : order;
-    }
-    u64 bound = (u64)reached(mine, (k + run - 1) / run, largest) << 32;
-    bound = bound ? bound : 1;
-    constexpr int kEach = 4;  // keys a thread at a time
-    static_assert(kEach * kTopThreads <= kKeys / 2, "room after every cut");
-    int have = 0;
-    for (int from = 0; from < n; from += kEach * kTopThreads) {
-        u64 key[kEach];
-        int more = 0, total;
+    u64 key[kEach];
+    auto request = [&](int from) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int at = from + i * kTopThreads + threadIdx.x;
             key[i] = at < n ? best[at] : 0;
-            more += key[i] >= bound;
         }
+    };
+    request(0);
+    u64 most = 0;
+    int reach = k;
+    if (n <= kAtOnce) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) most = key[i] > most ? key[i] : most;
+    } else {
+        const int run = k < 4 ? 1 : 4, runs = k / run;  // (of a part; keys behind are in none)
+        reach = (k + run - 1) / run;
+        for (int i = threadIdx.x; i < parts * runs; i += kTopThreads) {
+            const int part = i / runs;
+            const u64 last = best[part * k + (i - part * runs) * run + run - 1];
+            most = last > most ? last : most;
+        }
+    }
+    u64 bound = (u64)reached((uint32_t)(most >> 32), reach, largest) << 32;
+    bound = bound ? bound : 1;
+    int have = 0;
+    for (int from = 0; from < n; from += kAtOnce) {
+        if (from) request(from);
+        int more = 0, total;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) more += key[i] >= bound;
         int to = places(more, have, kept.in_wave[0][0], total);
 #pragma unroll
         for (int i = 0; i < kEach; ++i)

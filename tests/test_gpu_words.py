@@ -897,3 +897,21 @@ def test_smallest_scores(state):
         want = ow.top(x, k)
         np.testing.assert_array_equal(word.cpu().numpy(), want[0])
         np.testing.assert_array_equal(value.cpu().numpy(), want[1])
+
+
+@pytest.mark.parametrize("k", [1, 3, 5, 200, 256])
+def test_top_of_many_parts(state, k):
+    """A row of more parts than a workgroup has threads, with ties and with parts that hold
+    fewer than k words."""
+    say(f"top {k} of 5 000 000 words")
+    V = 5000000
+    x = torch.empty((2, V), device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(k))
+    x[0] = (x[0] * 8).round()  # (many ties)
+    x[1, 100000:4900000] = -np.inf
+    word = torch.empty((2, k), dtype=torch.int32, device="cuda")
+    value = torch.empty((2, k), device="cuda")
+    sp.spdp_top(state.h, x, word, value, work_for(2, V, k))
+    for i, row in enumerate(x.cpu().numpy()):
+        want = np.argsort(-row, kind="stable")[:k]
+        np.testing.assert_array_equal(word[i].cpu().numpy(), want)
+        np.testing.assert_array_equal(value[i].cpu().numpy(), row[want])
