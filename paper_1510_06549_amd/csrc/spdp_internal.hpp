@@ -358,8 +358,8 @@ constexpr int32_t kBlock8 = SPDP_BLOCK8;
 constexpr int64_t kStreamBytes = 64 << 20;    // scores above it are streamed past the caches
 // Bytes of scores that spdp_predict holds at a time, and what its documents at a time are a
 // multiple of.  Launches and words read again cost more than what the caches save: the best
-// words of 2 000 documents (100 000 words, 500 topics, fp32) take 983 us with 48 MB at a
-// time, 787 with 96, 702 with 400 and 640 with all 800.
+// words of 2 000 documents (100 000 words, 500 topics, fp32) take 877 us with 48 MB at a
+// time, 673 with 128, 591 with 400 and 537 with all 800.
 constexpr int64_t kPredictScores = 512 << 20;
 constexpr int64_t kPredictTile = 128;
 // Workgroups of a launch, of up to 512 threads: a launch counts threads in 32 bits.  More rows

@@ -503,6 +503,72 @@ def _vector(x, shape, dtype, what):
     return x.data_ptr()
 
 
+class _Device:
+    """Device memory from the library's own HIP runtime, with what these calls ask of a tensor:
+    for calls on host arrays, in programs that may have no tensor library (or have one that
+    would bring a second runtime, were it loaded now)."""
+
+    _SIZES = {"float64": 8, "int64": 8, "float32": 4, "int32": 4, "float8_e4m3fn": 1, "uint8": 1}
+    is_cuda = True
+
+    def __init__(self, shape, dtype, host=None):
+        self.shape, self.dtype, self.ptr = tuple(int(n) for n in shape), "torch." + dtype, None
+        self.size = self._SIZES[dtype]
+        if self.numel():
+            p = C.c_void_p()
+            self._hip("hipMalloc", C.byref(p), C.c_size_t(self.numel() * self.size))
+            self.ptr = p
+            if host is not None:
+                host = np.ascontiguousarray(host, dtype)
+                assert host.size == self.numel()
+                self._hip("hipMemcpy", p, C.c_void_p(host.ctypes.data), C.c_size_t(host.nbytes),
+                          C.c_int(1))
+
+    @staticmethod
+    def _hip(name, *args):
+        rc = getattr(lib(), name)(*args)
+        if rc:
+            raise SpdpError(SPDP_E_HIP, f"{name}: HIP error {rc}")
+
+    @classmethod
+    def wait(cls):
+        cls._hip("hipDeviceSynchronize")
+
+    def host(self):
+        out = np.empty(self.shape, self.dtype[6:])
+        if self.ptr:
+            self._hip("hipMemcpy", C.c_void_p(out.ctypes.data), self.ptr, C.c_size_t(out.nbytes),
+                      C.c_int(2))
+        return out
+
+    def __del__(self):
+        if self.ptr:
+            lib().hipFree(self.ptr)
+            self.ptr = None
+
+    def data_ptr(self):
+        return self.ptr.value if self.ptr else 0
+
+    def numel(self):
+        n = 1
+        for m in self.shape:
+            n *= m
+        return n
+
+    def element_size(self):
+        return self.size
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:], dtype=np.int64))
+                     for i in range(len(self.shape)))
+
+    def is_contiguous(self):
+        return True
+
+
 class Rows8:
     """Rows in 8 bits: q [rows, blocks * 128] (torch.float8_e4m3fn) and e [rows, blocks]
     (uint8, exponent + 127 of each block's scale); see include/spdp.h."""
@@ -801,42 +867,47 @@ class Sampler:
         probabilities).  doc_words: a list of word ids for every document, which `penalties`
         = (repeat, presence, frequency) make less likely; bias [V]: added to the scores;
         allowed [V]: truth values, the words to choose from."""
-        import torch
-
-        dev = torch.device("cuda", torch.cuda.current_device())
-        put = lambda x, t: torch.as_tensor(np.ascontiguousarray(x, t)).to(dev)  # noqa: E731
+        theta, phi = np.asarray(theta, np.float64), np.asarray(phi, np.float64)
+        if theta.ndim != 2 or phi.ndim != 2 or theta.shape[1] != phi.shape[1]:
+            raise ValueError("theta [D, K] and phi [V, K]")
         D, V = len(theta), len(phi)
+
+        def put(x, dtype):
+            x = np.asarray(x, dtype)
+            return _Device(x.shape, dtype, x)
+
         rules = None
         if doc_words is not None or bias is not None or allowed is not None:
             r = {}
             if doc_words is not None:
                 if len(doc_words) != D:
                     raise ValueError("doc_words: one list per document")
-                r["doc_off"] = put(np.cumsum([0] + [len(w) for w in doc_words]), np.int64)
+                r["doc_off"] = put(np.cumsum([0] + [len(w) for w in doc_words]), "int64")
                 r["words"] = put(np.concatenate([np.asarray(w, np.int32) for w in doc_words] +
-                                                [np.empty(0, np.int32)]), np.int32)
+                                                [np.empty(0, np.int32)]), "int32")
                 r["penalties"] = put(np.broadcast_to(np.asarray(penalties, np.float32), (D, 3)),
-                                     np.float32)
+                                     "float32")
             if bias is not None:
-                r["bias"] = put(np.reshape(bias, (1, V)), np.float32)
+                r["bias"] = put(np.reshape(bias, (1, V)), "float32")
             if allowed is not None:
                 bits = np.zeros(-(-V // 32) * 32, np.uint8)
                 bits[:V] = np.asarray(allowed, bool)
-                r["mask"] = put(np.packbits(bits, bitorder="little").view("<i4")[None], np.int32)
+                r["mask"] = put(np.packbits(bits, bitorder="little").view("<i4")[None], "int32")
             rules = Rules(D, V, **r)
         packed = []
         for x in (theta, phi):
-            x = put(x, np.float64)
-            packed.append((x, Rows8.empty(*x.shape, device=dev)))
-        outs = [tuple(torch.empty((D, n), dtype=t, device=dev)
-                      for t in (torch.int32, torch.float32)) for n in (top, draws)]
-        work = torch.empty(spdp_predict_work(D, V, torch.float32, top), dtype=torch.uint8,
-                           device=dev)
-        torch.cuda.synchronize(dev)  # (the state's stream may be another than torch's)
-        for x, to in packed:
-            spdp_pack8(self.h, x, to)
-        spdp_predict(self.h, packed[0][1], packed[1][1], work, rules=rules,
-                     top=outs[0] if top else None, drawn=outs[1] if draws else None,
-                     temperature=temperature, seed=seed, step=step)
-        torch.cuda.synchronize(dev)
-        return tuple(x.cpu().numpy() for pair in outs for x in pair)
+            nb = -(-x.shape[1] // SPDP_BLOCK8)
+            packed.append(Rows8(_Device((len(x), nb * SPDP_BLOCK8), "float8_e4m3fn"),
+                                _Device((len(x), nb), "uint8"), x.shape[1]))
+        given = [put(x, "float64") for x in (theta, phi)]
+        outs = [(_Device((D, n), "int32"), _Device((D, n), "float32")) for n in (top, draws)]
+        work = _Device((spdp_predict_work(D, V, "torch.float32", top),), "uint8")
+        try:
+            for x, to in zip(given, packed):
+                spdp_pack8(self.h, x, to)
+            spdp_predict(self.h, packed[0], packed[1], work, rules=rules,
+                         top=outs[0] if top else None, drawn=outs[1] if draws else None,
+                         temperature=temperature, seed=seed, step=step)
+        finally:
+            _Device.wait()  # (before the memory is given back)
+        return tuple(x.host() for pair in outs for x in pair)

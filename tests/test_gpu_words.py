@@ -11,6 +11,9 @@ hardware's base-2 logarithm, its scaling and their roundings); then half a step 
 output's type.
 """
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -786,12 +789,42 @@ def test_predict_of_a_trained_state():
     s.close()
 
 
-def test_captured_and_on_streams():
+def test_predict_without_a_tensor_library():
+    """In a program that has loaded the library only, whose HIP runtime is not torch's."""
+    say("predict in a process of its own")
+    code = """
+import sys
+import numpy as np
+from paper_1510_06549_amd import spdp as sp
+s = sp.Sampler(np.array([0, 1], np.int32), np.array([0, 2], np.int64), np.array([0], np.int32),
+               1, 2, 1, 0.1, 0.5, 1.0, 0.1)
+s.sweep(0, 1)
+rng = np.random.default_rng(0)
+theta, phi = rng.random((3, 7)), rng.random((600, 7))
+theta, phi = np.round(theta * 8 + 1), np.round(phi * 8 + 1)  # (exact in 8 bits)
+word, value, drawn, logp = s.predict(theta, phi, top=5, draws=4, seed=3)
+exact = theta @ phi.T
+want = np.argsort(-exact, axis=1, kind='stable')[:, :5]
+assert np.array_equal(word, want), (word, want)
+assert np.allclose(np.exp(value), np.take_along_axis(exact, want, 1), rtol=1e-5)
+assert drawn.shape == (3, 4) and (drawn >= 0).all() and (drawn < 600).all()
+assert [x.shape for x in s.predict(theta[:0], phi, top=5)] == [(0, 5), (0, 5), (0, 0), (0, 0)]
+s.close()
+assert 'torch' not in sys.modules
+print('ok')
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100,
+                          cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0 and done.stdout.strip() == "ok", done.stderr[-2000:]
+
+
+@pytest.mark.parametrize("V", [5000, 20000])
+def test_captured_and_on_streams(V):
     """A captured chain, replayed between eager calls with other inputs, and two states on
     streams of their own with workspaces of their own."""
     say("captured words")
     rng = np.random.default_rng(12)
-    D, V, K = 20, 5000, 60
+    D, K = 20, 60
     stream = torch.cuda.Stream()
     s, e = _state(stream), _state()
     theta = [dev(rng.dirichlet(np.full(K, 0.2), size=D)) for _ in range(3)]
@@ -802,11 +835,14 @@ def test_captured_and_on_streams():
     def chain(h, x, packed, work, outs):
         sp.spdp_pack8(h, x, packed)
         sp.spdp_predict(h, packed, words, work, rules=r.c, top=outs[0], drawn=outs[1], u=u)
+        sp.spdp_product8(h, packed, words, outs[2][0])
+        sp.spdp_adjust(h, outs[2][0], r.c, outs[2][0])
 
     def room():
         return (sp.Rows8.empty(D, K), torch.empty(sp.spdp_predict_work(D, V, torch.float32, 20),
                                                   dtype=torch.uint8, device="cuda"),
-                (_outs(D, 20), _outs(D, 9)))
+                (_outs(D, 20), _outs(D, 9),
+                 (torch.empty((D, V), dtype=torch.float16, device="cuda"),)))
 
     x = theta[0].clone()
     mine, other = room(), room()
@@ -820,7 +856,7 @@ def test_captured_and_on_streams():
             graph.replay()
         chain(e.h, t, *other)  # at the same time, on the null stream
         torch.cuda.synchronize()
-        for a, b in zip(mine[2][0] + mine[2][1], other[2][0] + other[2][1]):
+        for a, b in zip(sum(mine[2], ()), sum(other[2], ())):
             assert torch.equal(a.nan_to_num(5.0), b.nan_to_num(5.0))
     s.close()
     e.close()
