@@ -945,8 +945,8 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
     }
 }
 
-// One workgroup per (row, chunk): its largest score and its sums.  Rows of one chunk (ONE) are
-// drawn from at once.
+// One workgroup per (row, chunk): its largest score and its sums.  From rows of one chunk the
+// workgroup draws at once (ONE).
 //
 // 500 x 100 000 in bf16 (100 MB): 52 us, 65 with rules.  The scores' bytes would take 22:
 // what bounds it are 30 vector instructions for each score, 13 of them in fp64, which issue
@@ -1114,6 +1114,13 @@ TopShape top_shape(int64_t rows, int64_t V)
 
 int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 
+// Rows of one chunk: a row's own workgroup (eight wavefronts, 64 draws each at a time) makes up
+// to kDrawAlone draws, and more where there are kRowsAlone rows to fill the chip; else many
+// wavefronts do, in a second launch.  (5 000 words, us alone and by many: 1 row, 256 draws 14
+// and 11, 1 000 draws 35 and 11; 32 rows, 256 draws 14 and 17, 1 000 draws 36 and 17; 256
+// rows, 1 000 draws 37 and 37; 512 rows, 1 000 draws 51 and 60.)
+constexpr int64_t kDrawAlone = 384, kRowsAlone = 256;
+
 // (250 draws of 500 rows without rules: 79 us in all with 16 384 wavefronts, 74 with 8 192,
 // 76 with 4 096)
 constexpr int64_t kDrawWaves = 8192;
@@ -1150,8 +1157,9 @@ int64_t words_work(int64_t rows, int64_t V, int32_t take)
     const int64_t parts = most < rows + kTopBlocks ? most : rows + kTopBlocks;
     const int64_t chunks = chunks_of(V, kDrawChunk);
     const int64_t top = parts * take * (int64_t)sizeof(u64);
-    const int64_t draw = chunks > 1 ? draw_parts_bytes(rows, chunks) + rows * chunks * kSums * 8 : 0;
-    return round256(top > draw ? top : draw > 0 ? draw : 1);
+    const int64_t apart = chunks > 1 || rows < kRowsAlone ? rows : kRowsAlone;
+    const int64_t draw = draw_parts_bytes(apart, chunks) + apart * chunks * kSums * 8;
+    return round256(top > draw ? top : draw);
 }
 
 hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
@@ -1191,14 +1199,15 @@ hipError_t launch_draw(const void *x, int64_t ld, int32_t type, int64_t rows, in
         const spdp_rules r = rules_from(rules, row);
         const int64_t at = row * draws;
         const double *given = u ? u + at : nullptr;
+        const bool alone = chunks == 1 && (draws <= kDrawAlone || m >= kRowsAlone);
         const hipError_t e = by_type(type, m * chunks, [&](auto t, dim3 grid) {
             using T = decltype(t);
-            const auto kernel = chunks == 1 ? k_draw_parts<T, true> : k_draw_parts<T, false>;
+            const auto kernel = alone ? k_draw_parts<T, true> : k_draw_parts<T, false>;
             hipLaunchKernelGGL(kernel, grid, dim3(kDrawThreads), 0, st, (const T *)from, ld, V,
                                (int32_t)chunks, r, scale, part, sums, draws, given, seed, step,
                                draw0 + at, word + at, logp + at);
         });
-        if (e != hipSuccess || chunks == 1) return e;
+        if (e != hipSuccess || alone) return e;
         // a wavefront per draw while that does not fill the chip, then several each
         int64_t waves = (kDrawWaves + m - 1) / m;
         waves = waves > draws ? draws : waves;

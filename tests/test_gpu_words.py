@@ -521,6 +521,29 @@ def test_draw_from_long_documents(state, V, lens):
                  ow.adjusted(x.cpu().numpy(), docs, pen), u, 1.0)
 
 
+@pytest.mark.parametrize("rows,n", [(1, 384), (1, 385), (2, 5000), (255, 400), (256, 400)])
+def test_many_draws(state, rows, n):
+    """Draws of rows of one chunk, by the row's own workgroup or by several."""
+    say(f"draw {n} of {rows} x 3000")
+    rng = np.random.default_rng(rows + n)
+    V = 3000
+    x = _scores(rng, rows, V, torch.float32)
+    r = RuleSet(rng, rows, V)
+    u = rng.random((rows, n))
+    u[0, 7] = 1.0
+    word, wbuf = framed(rows, n, torch.int32, fill=9)
+    logp, lbuf = framed(rows, n, torch.float32)
+    sp.spdp_draw(state.h, x, word, logp, work_for(rows, V), u=dev(u), rules=r.c)
+    some = np.r_[0:min(rows, 3), rows - min(rows, 3):rows]
+    xo = r.oracle(x)
+    last = np.flatnonzero(xo[0] > -np.inf)
+    assert word[0, 7].item() == (last[-1] if len(last) else -1)
+    word[0, 7], logp[0, 7] = word[0, 8].clone(), logp[0, 8].clone()
+    u[0, 7] = u[0, 8]
+    _check_draws(word[dev(some)].cpu().numpy(), logp[dev(some)].cpu().numpy(), xo[some], u[some], 1.0)
+    assert frame_kept(wbuf, word, 9) and frame_kept(lbuf, logp)
+
+
 def test_draw_of_many_chunks(state):
     """More chunks than a wavefront has lanes, some of them without weight, the last among
     them, and more draws than it makes at a time."""
