@@ -358,8 +358,9 @@ int spdp_pack8(spdp_state *s, const void *x, int32_t type, int64_t ld, const spd
  * elements exact (bf16, which holds them for scales of 2^-124 to 2^119; beyond, they
  * round to bf16 or become infinite) and sums in fp32, or its natural logarithm if
  * log_scores != 0 (-inf where the sum is 0, NaN where it is negative), rounded to `type` (SPDP_F32, SPDP_F16 or SPDP_BF16).  c is
- * device [a->rows][b->rows] with ld elements from one row to the next; elements
- * behind a row's end are left as they are.
+ * device [a->rows][b->rows] with ld elements from one row to the next (rows that
+ * start at multiples of 64 bytes are written fastest); elements behind a row's end are
+ * left as they are.
  * Errors: E_ARG (NULL pointer, sizes out of range or columns that differ, ld <
  * b->rows, another type, buffers as for spdp_pack8), E_HIP.
  */

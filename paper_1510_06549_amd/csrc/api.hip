@@ -1202,11 +1202,18 @@ int check_draws(const spdp_state *s, int32_t draws, double temperature, int64_t 
     return check_device(s, logp, rows * draws * 4, 4, "logp");
 }
 
-// Workspace of spdp_predict for `rows` documents at a time: their scores (unless
-// the caller keeps them), then what choosing words needs.
+// Workspace of spdp_predict for `rows` documents at a time: their scores (unless the
+// caller keeps them), in rows of whole 64 bytes (which the product writes fastest), then what
+// choosing words needs.
+int64_t scores_pitch(int64_t n, int32_t type)
+{
+    const int64_t unit = 64 / type_size(type);
+    return (n + unit - 1) / unit * unit;
+}
+
 int64_t scores_room(int64_t rows, int64_t n, int32_t type, bool kept)
 {
-    return kept ? 0 : (rows * n * type_size(type) + 255) / 256 * 256;
+    return kept ? 0 : (rows * scores_pitch(n, type) * type_size(type) + 255) / 256 * 256;
 }
 
 }  // namespace
@@ -1315,7 +1322,7 @@ int spdp_predict_work(int64_t docs, int32_t n_words, int32_t type, int32_t k, in
         return fail(SPDP_E_ARG, "size out of range");
     if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
         return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
-    int64_t rows = kPredictScores / (n_words * type_size(type));
+    int64_t rows = kPredictScores / (scores_pitch(n_words, type) * type_size(type));
     rows = rows < 1 ? 1 : rows > kPredictTile ? rows - rows % kPredictTile : rows;
     rows = rows < docs ? rows : docs;
     *bytes = scores_room(rows, n_words, type, false) + words_work(rows, n_words, k);
@@ -1364,7 +1371,7 @@ int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
     for (int64_t d = 0; d < D; d += rows) {
         const int64_t m = rows < D - d ? rows : D - d;
         const spdp_rows8 part{m, docs->cols, docs->q + d * blocks * kBlock8, docs->e + d * blocks};
-        const int64_t ld = kept ? a.ld : V;
+        const int64_t ld = kept ? a.ld : scores_pitch(V, a.type);
         void *x = kept ? static_cast<char *>(a.scores) + d * ld * type_size(a.type) : work;
         void *rest = static_cast<char *>(work) + scores_room(rows, V, a.type, kept);
         HIP_TRY(launch_product8(part, *words, true, x, a.type, ld, s->st));

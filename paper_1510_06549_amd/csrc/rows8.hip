@@ -452,21 +452,24 @@ __global__ void __launch_bounds__(256) k_product8_few(
 }
 
 // How a product is shared out: document tiles, workgroups that share a document
-// tile's words, and the rounds of words that each of their wavefronts takes.
+// tile's words, the rounds of words that each of their wavefronts takes, and what that
+// costs.  A compute unit takes `turns` workgroups one after another; a round takes as long
+// as its products or 3 more document fragments' (its words' conversion and stores), a
+// workgroup's start as long as 2 of them.
 struct Shares {
-    int64_t tiles_d, ranges, rounds;
+    int64_t tiles_d, ranges, rounds, cost;
 };
 
-Shares shares_of(int64_t m, int64_t n, int32_t fd)
+Shares shares_of(int64_t m, int64_t n, int32_t fd, int64_t turns)
 {
     const int64_t tw = (n + 16 * kWordFragments - 1) / (16 * kWordFragments), most = (tw + 7) / 8;
     Shares s;
     s.tiles_d = (m + 16 * fd - 1) / (16 * fd);
-    // a workgroup for each of the 256 compute units; where there are several times as
-    // many tiles of documents, some more, to end together
-    s.ranges = s.tiles_d <= 32 ? 256 / s.tiles_d : (1024 + s.tiles_d - 1) / s.tiles_d;
+    s.ranges = 256 * turns / s.tiles_d;
     if (s.ranges > most) s.ranges = most;
+    if (s.ranges < 1) s.ranges = 1;
     s.rounds = (tw + 8 * s.ranges - 1) / (8 * s.ranges);
+    s.cost = (s.tiles_d * s.ranges + 255) / 256 * (s.rounds * (fd + 3) + 2);
     return s;
 }
 
@@ -474,12 +477,15 @@ Shares shares_of(int64_t m, int64_t n, int32_t fd)
 // the words, which every tile of documents reads again (2 000 x 100 000 in bf16, 400 MB: 237
 // us, 192 streamed; 1 000 x 100 000 of 64 topics in fp16, 200 MB: 72 and 56 us).  Less than
 // that stays in the last level cache for whoever reads it next, and takes less time too (777
-// x 14 724 in fp16, 23 MB: 11.2 us, 15.0 streamed).
+// x 14 724 in fp16, 23 MB: 11.2 us, 15.0 streamed).  Rows have to start at multiples of 64
+// bytes: lines that are written in parts are not put together past the caches (2 000 x 99 999
+// of 500 topics in bf16: 384 us streamed, 272 not; 2 000 x 100 016, rows at multiples of 32
+// bytes: 256 and 233, of 700 topics 296 and 340).
 template <typename T, bool LOG, int FD, bool STREAM>
-hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
+hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, const Shares &s,
+                   hipStream_t st)
 {
     const int32_t nb = blocks8(a.cols), held = nb < kLdsBlocks / FD ? nb : kLdsBlocks / FD;
-    const Shares s = shares_of(a.rows, b.rows, FD);
     const int64_t per = (s.tiles_d * s.ranges + 7) / 8;
     hipLaunchKernelGGL((k_product8<T, LOG, FD, STREAM>), dim3((unsigned)(per * 8)), dim3(512),
                        held * FD * 4096, st, a.q, a.e, (int32_t)a.rows, b.q, b.e, (int32_t)b.rows,
@@ -488,16 +494,16 @@ hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld
 }
 
 template <typename T, bool LOG, int FD>
-hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
+hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, const Shares &s,
+                   hipStream_t st)
 {
-    return a.rows * b.rows * (int64_t)sizeof(T) > kStreamBytes
-               ? product<T, LOG, FD, true>(a, b, c, ld, st)
-               : product<T, LOG, FD, false>(a, b, c, ld, st);
+    const bool lines = ((uintptr_t)c | (uintptr_t)(ld * (int64_t)sizeof(T))) % 64 == 0;
+    return lines && a.rows * b.rows * (int64_t)sizeof(T) > kStreamBytes
+               ? product<T, LOG, FD, true>(a, b, c, ld, s, st)
+               : product<T, LOG, FD, false>(a, b, c, ld, s, st);
 }
 
-// Document fragments of a workgroup: those with which the longest wavefront has the
-// least to do, a round taking as long as its products or 3 more document fragments' (its
-// words' conversion and stores).
+// Document fragments of a workgroup and turns: those that cost least.
 template <typename T, bool LOG>
 hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, hipStream_t st)
 {
@@ -509,21 +515,20 @@ hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld
         return hipGetLastError();
     }
     int32_t best = 0;
-    int64_t least = INT64_MAX;
-    for (int32_t fd : {2, 4, 6, 8}) {
-        const Shares s = shares_of(a.rows, b.rows, fd);
-        const int64_t over = (s.tiles_d * s.ranges + 255) / 256;
-        const int64_t cost = s.rounds * over * (fd + 3);
-        if (cost < least) {
-            least = cost;
-            best = fd;
+    Shares s{};
+    for (int32_t fd : {2, 4, 6, 8})
+        for (int64_t turns = 1; turns <= 8; ++turns) {
+            const Shares o = shares_of(a.rows, b.rows, fd, turns);
+            if (!best || o.cost < s.cost) {
+                s = o;
+                best = fd;
+            }
         }
-    }
     switch (best) {
-        case 2: return product<T, LOG, 2>(a, b, c, ld, st);
-        case 4: return product<T, LOG, 4>(a, b, c, ld, st);
-        case 6: return product<T, LOG, 6>(a, b, c, ld, st);
-        default: return product<T, LOG, 8>(a, b, c, ld, st);
+        case 2: return product<T, LOG, 2>(a, b, c, ld, s, st);
+        case 4: return product<T, LOG, 4>(a, b, c, ld, s, st);
+        case 6: return product<T, LOG, 6>(a, b, c, ld, s, st);
+        default: return product<T, LOG, 8>(a, b, c, ld, s, st);
     }
 }
 
