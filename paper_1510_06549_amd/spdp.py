@@ -542,9 +542,12 @@ class _Device:
         return out
 
     def __del__(self):
-        if self.ptr:
-            lib().hipFree(self.ptr)
-            self.ptr = None
+        try:
+            if self.ptr:
+                lib().hipFree(self.ptr)
+                self.ptr = None
+        except Exception:
+            pass
 
     def data_ptr(self):
         return self.ptr.value if self.ptr else 0
