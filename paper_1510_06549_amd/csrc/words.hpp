@@ -64,28 +64,36 @@ struct RowRules {
 
 __device__ __forceinline__ RowRules row_rules(const spdp_rules &r, int64_t row)
 {
-    RowRules o;
+    // everything that is read of the row is requested before any of it is looked at
+    int64_t a = 0, b = 0;
+    float repeat = 1.f, presence = 0.f, frequency = 0.f;
+    int32_t bias = 0, mask = 0;
     if (r.doc_off) {
-        int64_t a = r.doc_off[row], b = r.doc_off[row + 1];
-        a = a < 0 ? 0 : a;
-        b = b > r.n_listed ? r.n_listed : b;
-        if (a < b) {
-            o.words = r.words + a;
-            o.n_words = b - a;
-            o.repeat = r.penalties[3 * row];
-            o.presence = r.penalties[3 * row + 1];
-            o.frequency = r.penalties[3 * row + 2];
-        }
+        a = r.doc_off[row];
+        b = r.doc_off[row + 1];
+        repeat = r.penalties[3 * row];
+        presence = r.penalties[3 * row + 1];
+        frequency = r.penalties[3 * row + 2];
+    }
+    if (r.bias_of) bias = r.bias_of[row];
+    if (r.mask_of) mask = r.mask_of[row];
+    RowRules o;
+    a = a < 0 ? 0 : a;
+    b = b > r.n_listed ? r.n_listed : b;
+    if (a < b) {
+        o.words = r.words + a;
+        o.n_words = b - a;
+        o.repeat = repeat;
+        o.presence = presence;
+        o.frequency = frequency;
     }
     if (r.bias) {
-        const int32_t k = r.bias_of ? r.bias_of[row] : 0;
-        if (k >= r.n_bias) o.bad = true;
-        else if (k >= 0) o.bias = r.bias + (int64_t)k * r.n_words;
+        if (bias >= r.n_bias) o.bad = true;
+        else if (bias >= 0) o.bias = r.bias + (int64_t)bias * r.n_words;
     }
     if (r.mask) {
-        const int32_t k = r.mask_of ? r.mask_of[row] : 0;
-        if (k >= r.n_masks) o.bad = true;
-        else if (k >= 0) o.mask = r.mask + (int64_t)k * (((int64_t)r.n_words + 31) / 32);
+        if (mask >= r.n_masks) o.bad = true;
+        else if (mask >= 0) o.mask = r.mask + (int64_t)mask * (((int64_t)r.n_words + 31) / 32);
     }
     return o;
 }
