@@ -135,7 +135,13 @@ __device__ __forceinline__ T out_as(float v);
 template <>
 __device__ __forceinline__ float out_as<float>(float v) { return v; }
 template <>
-__device__ __forceinline__ _Float16 out_as<_Float16>(float v) { return (_Float16)v; }
+__device__ __forceinline__ _Float16 out_as<_Float16>(float v)
+{
+    // (the value is rounded to fp32 first: a multiplication and the conversion in one instruction
+    // would round once, here and there, and the kernels' results would differ)
+    asm("" : "+v"(v));
+    return (_Float16)v;
+}
 template <>
 __device__ __forceinline__ __bf16 out_as<__bf16>(float v) { return (__bf16)v; }
 

@@ -652,6 +652,20 @@ def test_product_does_not_depend_on_the_batch(state, n):
         assert torch.equal(sp.spdp_product8(state.h, part, b8, out, log=True), whole[i:j]), (i, j)
 
 
+@pytest.mark.parametrize("m", [1, 6, 60, 300])
+def test_product_in_16_bits_is_the_rounded_one(state, m):
+    """In every kernel: fp32 first, then the output's type, with nothing rounded in between."""
+    say(f"product: {m} documents in 16 bits")
+    rng = np.random.default_rng(m)
+    theta, phi = rng.dirichlet(np.full(8, 0.1), size=m), rng.random((100001, 8)) ** 8 + 1e-9
+    a, b = (sp.spdp_pack8(state.h, dev(x), sp.Rows8.empty(*x.shape)) for x in (theta, phi))
+    for log in (False, True):
+        want = sp.spdp_product8(state.h, a, b, torch.empty((m, 100001), device="cuda"), log=log)
+        for t in (torch.float16, torch.bfloat16):
+            got = torch.empty((m, 100001), dtype=t, device="cuda")
+            assert torch.equal(sp.spdp_product8(state.h, a, b, got, log=log), want.to(t)), (t, log)
+
+
 # ---------------------------------------------------------------------------
 # refusals that need a device
 # ---------------------------------------------------------------------------
@@ -974,3 +988,31 @@ def test_top_of_many_parts(state, k):
         want = np.argsort(-row, kind="stable")[:k]
         np.testing.assert_array_equal(word[i].cpu().numpy(), want)
         np.testing.assert_array_equal(value[i].cpu().numpy(), row[want])
+
+
+def test_more_scores_than_32_bits_count(state):
+    """The last documents of 2.2e9 scores have the words that they have alone."""
+    say("22 000 x 100 001 scores")
+    rng = np.random.default_rng(9)
+    D, V, K, tail = 22000, 100001, 8, 6
+    assert D * V > 1 << 31
+    docs, words = (sp.spdp_pack8(state.h, dev(x), sp.Rows8.empty(*x.shape)) for x in
+                   (rng.dirichlet(np.full(K, 0.1), size=D), rng.dirichlet(np.full(V, 0.05), K).T + 1e-9))
+    last = sp.Rows8(docs.q[-tail:].contiguous(), docs.e[-tail:].contiguous(), K)
+    bias = torch.empty((1, V), device="cuda").normal_()
+    few, all_ = (sp.Rules(n, V, bias=bias) for n in (tail, D))
+    got, want = [], []
+    for d, n, r, to in ((docs, D, all_, got), (last, tail, few, want)):
+        x = torch.empty((n, V), dtype=torch.float16, device="cuda")
+        sp.spdp_product8(state.h, d, words, x, log=True)
+        sp.spdp_adjust(state.h, x, r, x)
+        u = torch.full((n, 7), 0.6, dtype=torch.float64, device="cuda")
+        u[:, 3] = 0.01
+        w = work_for(n, V, 9)
+        top, drawn = _outs(n, 9), _outs(n, 7)
+        sp.spdp_top(state.h, x, *top, w)
+        sp.spdp_draw(state.h, x, *drawn, w, u=u)
+        to += [t[-tail:].clone() for t in (x, *top, *drawn)]
+        del x
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert (got[1] >= 0).all() and (got[3] >= 0).all()
