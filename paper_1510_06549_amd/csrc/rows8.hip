@@ -206,7 +206,7 @@ __device__ __forceinline__ void store_unit(T *p, i4v v)
 // Columns past kLdsBlocks / FD blocks do not fit the LDS at once: then documents are
 // staged again, part by part, for every round of words.
 //
-// 2 000 x 100 000 x 500 (512 padded) to logarithms in bf16: 181 us, 1 130 TFLOP/s of the
+// 2 000 x 100 000 x 500 (512 padded) to logarithms in bf16: 179 us, 1 140 TFLOP/s of the
 // padded products; 137 us without stores and logarithms, where a large product of the library
 // takes 140 at its best rate (1 430 TFLOP/s at 8 192 cubed, and 404 us for these sizes).  The
 // stores, 400 MB, and the logarithms run under other wavefronts' products only in part.

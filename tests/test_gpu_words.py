@@ -544,6 +544,22 @@ def test_many_draws(state, rows, n):
     assert frame_kept(wbuf, word, 9) and frame_kept(lbuf, logp)
 
 
+def test_draws_do_not_depend_on_their_company(state):
+    """The same uniforms draw the same words alone, with others and in other batches of rows."""
+    say("draw: alone and together")
+    rng = np.random.default_rng(77)
+    for V in (3000, 30000):
+        rows, n = 300, 1000
+        x = _scores(rng, rows, V, torch.bfloat16)
+        u = dev(rng.random((rows, n)))
+        word, logp = _outs(rows, n)
+        sp.spdp_draw(state.h, x, word, logp, work_for(rows, V), u=u)
+        for i, j, k in ((0, 1, 1000), (0, 1, 384), (5, 6, 1), (10, 40, 70), (0, 255, 999)):
+            w, p = _outs(j - i, k)
+            sp.spdp_draw(state.h, x[i:j], w, p, work_for(j - i, V), u=u[i:j, :k].contiguous())
+            assert torch.equal(w, word[i:j, :k]) and torch.equal(p, logp[i:j, :k]), (V, i, j, k)
+
+
 def test_draw_of_many_chunks(state):
     """More chunks than a wavefront has lanes, some of them without weight, the last among
     them, and more draws than it makes at a time."""
