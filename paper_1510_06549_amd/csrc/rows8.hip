@@ -43,12 +43,13 @@ __device__ __forceinline__ float scaled_odd(double x, int e)
 {
     const u64 bits = __builtin_bit_cast(u64, x);
     const uint32_t high = (uint32_t)(bits >> 32), low = (uint32_t)bits;
-    const int exponent = (int)(high >> 20 & 0x7FF) - e;  // of the scaled value, 1023 for 1
+    // of the scaled value, 1023 for 1; at most what fp32 has for infinities and NaN, where those
+    // of fp64 come out too
+    const int exponent = min((int)(high >> 20 & 0x7FF) - e, 1151);
     uint32_t f = (uint32_t)((bits & 0xFFFFFFFFFFFFFull) >> 29) | ((low & 0x1FFFFFFF) ? 1u : 0u);
     f |= (uint32_t)(exponent - 896) << 23;
     f = exponent < 1000 ? 0u : f;  // (below 2^-23)
-    const bool number = (high & 0x7FF00000u) != 0x7FF00000u && f <= 0x43E00000u;
-    f = number ? f : 0x7FC00000u;
+    f = f <= 0x43E00000u ? f : 0x7FC00000u;
     return __uint_as_float(f | (high & 0x80000000u));
 }
 

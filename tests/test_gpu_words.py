@@ -1032,3 +1032,21 @@ def test_more_scores_than_32_bits_count(state):
         del x
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert (got[1] >= 0).all() and (got[3] >= 0).all()
+
+
+def test_pack_every_power_of_two(state):
+    """All of fp64 from its least value to its largest, alone in a block and beside 1: beyond
+    448 2^127, the largest scale, there is no number."""
+    say("pack, every power of two of fp64")
+    two = np.ldexp(1.0, np.arange(-1074, 1024))
+    x = np.concatenate([two, -1.75 * two[:-1], 2.0 ** 127 * np.array(
+        [448.0, np.nextafter(448.0, 512.0), -448.0, -np.nextafter(448.0, 512.0)]),
+        [1e160, -1e195, 1.5 * 2.0 ** 640, 1.75 * 2.0 ** 647, np.finfo(np.float64).max]])
+    for beside in (False, True):
+        rows = np.stack([x, np.ones_like(x)], 1) if beside else x[:, None]
+        out = sp.Rows8.empty(*rows.shape)
+        sp.spdp_pack8(state.h, dev(rows), out)
+        q, e = ow.pack8(rows)
+        np.testing.assert_array_equal(out.e.cpu().numpy(), e)
+        np.testing.assert_array_equal(ow.value8(out.q.view(torch.uint8).cpu().numpy()),
+                                      ow.value8(q))
