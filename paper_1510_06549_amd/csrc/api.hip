@@ -1112,12 +1112,18 @@ int matrix_bytes(int64_t rows, int64_t n, int64_t ld, int32_t type, const char *
     return SPDP_OK;
 }
 
+int check_score_type(int32_t type)
+{
+    return type == SPDP_F32 || type == SPDP_F16 || type == SPDP_BF16
+               ? SPDP_OK
+               : fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+}
+
 // Rows of scores: their type, sizes and buffer.
 int check_scores(const spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t rows,
                  int64_t n, const char *name)
 {
-    if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
-        return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+    CALL(check_score_type(type));
     if (rows < 0 || rows > INT32_MAX || n < 1 || n > INT32_MAX)
         return fail(SPDP_E_ARG, "need 0 <= rows < 2^31 and 1 <= n_words < 2^31");
     int64_t bytes = 0;
@@ -1243,7 +1249,11 @@ int spdp_product8(spdp_state *s, const spdp_rows8 *a, const spdp_rows8 *b, int32
     CALL(check_rows8(s, b, "b"));
     if (a->cols != b->cols)
         return fail(SPDP_E_ARG, "rows of %d and %d columns", a->cols, b->cols);
-    if (b->rows == 0) return SPDP_OK;
+    if (b->rows == 0) {  // (nothing to write, but the same call otherwise)
+        int64_t bytes = 0;
+        CALL(check_score_type(type));
+        return matrix_bytes(0, 0, ld, type, "c", &bytes);
+    }
     CALL(check_scores(s, c, ld, type, a->rows, b->rows, "c"));
     OnDevice on(s->device);
     HIP_TRY(on.error());
@@ -1320,8 +1330,7 @@ int spdp_predict_work(int64_t docs, int32_t n_words, int32_t type, int32_t k, in
     if (!bytes) return fail(SPDP_E_ARG, "null argument");
     if (docs < 0 || docs > INT32_MAX || n_words < 1 || k < 0 || k > SPDP_MAX_TAKE)
         return fail(SPDP_E_ARG, "size out of range");
-    if (type != SPDP_F32 && type != SPDP_F16 && type != SPDP_BF16)
-        return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+    CALL(check_score_type(type));
     int64_t rows = kPredictScores / (scores_pitch(n_words, type) * type_size(type));
     rows = rows < 1 ? 1 : rows > kPredictTile ? rows - rows % kPredictTile : rows;
     rows = rows < docs ? rows : docs;
@@ -1343,8 +1352,7 @@ int spdp_predict(spdp_state *s, const spdp_rows8 *docs, const spdp_rows8 *words,
     if (V < 1) return fail(SPDP_E_ARG, "no words");
     const bool kept = a.scores != nullptr;
     if (kept) CALL(check_scores(s, a.scores, a.ld, a.type, D, V, "scores"));
-    else if (a.type != SPDP_F32 && a.type != SPDP_F16 && a.type != SPDP_BF16)
-        return fail(SPDP_E_ARG, "scores are SPDP_F32, SPDP_F16 or SPDP_BF16");
+    else CALL(check_score_type(a.type));
     if (rules) CALL(check_rules(s, rules, D, V));
     if (a.k != 0) CALL(check_take(s, a.k, D, a.top_word, a.top_value));
     if (a.draws != 0) CALL(check_draws(s, a.draws, a.temperature, D, a.u, a.draw_word, a.draw_logp));

@@ -170,3 +170,18 @@ def test_binding_wants_device_tensors():
                  torch.zeros(4, 2, dtype=torch.uint8), 200)
     with pytest.raises(ValueError):
         sp.Rules(4, 100, bias=torch.zeros(1, 100))
+
+
+@pytest.mark.parametrize("type,ld,text", [
+    (sp.SPDP_F64, 100, "SPDP_F32, SPDP_F16 or SPDP_BF16"),
+    (7, 100, "SPDP_F32, SPDP_F16 or SPDP_BF16"),
+    (-1, 0, "SPDP_F32, SPDP_F16 or SPDP_BF16"),
+    (sp.SPDP_F32, -1, "c: rows of 0 elements overlap at ld = -1"),
+])
+def test_product8_without_words(type, ld, text):
+    """A wrong call is refused where there is nothing to write, too."""
+    none = rows8(rows=0)
+    call = lambda *a: sp.lib().spdp_product8(  # noqa: E731
+        STATE, C.addressof(none), C.addressof(none), 0, P, *a)
+    refused(call(type, ld), text)
+    assert call(sp.SPDP_F16, 0) == sp.SPDP_OK
