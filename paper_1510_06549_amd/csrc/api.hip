@@ -1217,9 +1217,13 @@ int64_t scores_pitch(int64_t n, int32_t type)
     return (n + unit - 1) / unit * unit;
 }
 
+// (2^62, more than any device holds, for 2^62 and more: 2^31 rows of 2^31 scores pass 64 bits)
 int64_t scores_room(int64_t rows, int64_t n, int32_t type, bool kept)
 {
-    return kept ? 0 : (rows * scores_pitch(n, type) * type_size(type) + 255) / 256 * 256;
+    constexpr int64_t kMost = (int64_t)1 << 62;
+    const int64_t row = scores_pitch(n, type) * type_size(type);
+    if (kept) return 0;
+    return rows > (kMost - 255) / row ? kMost : (rows * row + 255) / 256 * 256;
 }
 
 }  // namespace
