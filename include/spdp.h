@@ -410,7 +410,11 @@ typedef struct {
 int spdp_adjust(spdp_state *s, const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
                 const spdp_rules *rules);
 
-/* Bytes of workspace that spdp_top (take = k) and spdp_draw need for their sizes. */
+/*
+ * Bytes of workspace that are enough for spdp_top (take = k) and for spdp_draw of these
+ * sizes.  Each is content with its own share: spdp_top with 8 k (rows + 1024) + 256 bytes at
+ * most, spdp_draw with 5136 bytes for every 8192 words begun of a row, and 512.
+ */
 int spdp_words_work(int64_t rows, int32_t n_words, int32_t take, int64_t *bytes);
 
 /*

@@ -1208,6 +1208,13 @@ int check_draws(const spdp_state *s, int32_t draws, double temperature, int64_t 
     return check_device(s, logp, rows * draws * 4, 4, "logp");
 }
 
+// Workspace for either of choosing words.
+int64_t words_work(int64_t rows, int64_t n, int32_t take)
+{
+    const int64_t top = top_work(rows, n, take), draw = draw_work(rows, n);
+    return top > draw ? top : draw;
+}
+
 // Workspace of spdp_predict for `rows` documents at a time: their scores (unless the
 // caller keeps them), in rows of whole 64 bytes (which the product writes fastest), then what
 // choosing words needs.
@@ -1304,7 +1311,7 @@ int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t row
     CALL(check_scores(s, x, ld, type, rows, n_words, "x"));
     if (rules) CALL(check_rules(s, rules, rows, n_words));
     CALL(check_take(s, k, rows, word, value));
-    CALL(check_work(s, work, work_bytes, words_work(rows, n_words, k)));
+    CALL(check_work(s, work, work_bytes, top_work(rows, n_words, k)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_top(x, ld, type, rows, n_words, rules ? *rules : spdp_rules{}, k, word, value,
@@ -1321,7 +1328,7 @@ int spdp_draw(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t ro
     CALL(check_scores(s, x, ld, type, rows, n_words, "x"));
     if (rules) CALL(check_rules(s, rules, rows, n_words));
     CALL(check_draws(s, draws, temperature, rows, u, word, logp));
-    CALL(check_work(s, work, work_bytes, words_work(rows, n_words, 0)));
+    CALL(check_work(s, work, work_bytes, draw_work(rows, n_words)));
     OnDevice on(s->device);
     HIP_TRY(on.error());
     HIP_TRY(launch_draw(x, ld, type, rows, n_words, rules ? *rules : spdp_rules{}, temperature,

@@ -384,7 +384,8 @@ hipError_t launch_product8(const spdp_rows8 &a, const spdp_rows8 &b, bool log, v
                            int32_t type, int64_t ld, hipStream_t st);
 hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32_t type,
                          int64_t rows, int64_t V, const spdp_rules &rules, hipStream_t st);
-int64_t words_work(int64_t rows, int64_t V, int32_t take);  // bytes for either of the next two
+int64_t top_work(int64_t rows, int64_t V, int32_t take);  // bytes of workspace
+int64_t draw_work(int64_t rows, int64_t V);
 hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,
                       const spdp_rules &rules, int32_t k, int32_t *word, float *value, void *work,
                       hipStream_t st);

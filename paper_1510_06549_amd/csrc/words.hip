@@ -1149,17 +1149,21 @@ hipError_t launch_adjust(const void *x, int64_t ldx, void *y, int64_t ldy, int32
     });
 }
 
-int64_t words_work(int64_t rows, int64_t V, int32_t take)
+int64_t top_work(int64_t rows, int64_t V, int32_t take)
 {
     if (rows == 0) return 0;
     // (at least what top_shape's parts need, and no less for more rows)
     const int64_t most = rows * chunks_of(V, kTopThreads * 16);
     const int64_t parts = most < rows + kTopBlocks ? most : rows + kTopBlocks;
+    return round256(parts * take * (int64_t)sizeof(u64));
+}
+
+int64_t draw_work(int64_t rows, int64_t V)
+{
+    if (rows == 0) return 0;
     const int64_t chunks = chunks_of(V, kDrawChunk);
-    const int64_t top = parts * take * (int64_t)sizeof(u64);
     const int64_t apart = chunks > 1 || rows < kRowsAlone ? rows : kRowsAlone;
-    const int64_t draw = draw_parts_bytes(apart, chunks) + apart * chunks * kSums * 8;
-    return round256(top > draw ? top : draw);
+    return round256(draw_parts_bytes(apart, chunks) + apart * chunks * kSums * 8);
 }
 
 hipError_t launch_top(const void *x, int64_t ld, int32_t type, int64_t rows, int64_t V,

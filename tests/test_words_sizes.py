@@ -67,3 +67,20 @@ for n in ((1 << 31) - 1, 3 << 29, 1 << 20, 1000):
         accepted(call(one))
         accepted(call(1 << 40))
 """)
+
+
+def test_workspaces_of_their_own(stand_in):
+    """Best words do not ask for the room that only draws use, nor draws for keys."""
+    run(stand_in, """
+for rows, n, k in ((20000, 100000, 10), (1, 100000, 1), (1024, 5000, 256), (1000000, 3, 256)):
+    ld, f32 = n, sp.SPDP_F32
+    top = lambda have: L.spdp_top(STATE, P, ld, f32, rows, n, None, k, P, P, P, have)
+    draw = lambda have: L.spdp_draw(STATE, P, ld, f32, rows, n, None, 1.0, 7, None, 0, 0, P, P, P, have)
+    both = sp.spdp_words_work(rows, n, k)
+    own = (min(both, 8 * k * (rows + 1024) + 256), min(both, 5136 * rows * -(-n // 8192) + 512))
+    for call, have in zip((top, draw), own):
+        accepted(call(both))
+        accepted(call(have))
+        refused(call(0), "a workspace of")
+    assert both <= max(8 * k * (rows + 1024) + 256, 5136 * rows * -(-n // 8192) + 512)
+""")
