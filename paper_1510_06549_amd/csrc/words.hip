@@ -852,6 +852,14 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
             }
             if (last || !__any(!found)) break;
         }
+        // A word has weight where it is above 2^-1075 beside the row's largest, which fp64 rounds to
+        // 0: beside its chunk's largest, above `least` (0 where that is the row's).
+        double least = 0.0;
+        if (chunks > 1 && __any(!(goal > 0.0))) {
+            least = power_of(-1075.0 * kPowers - (own - law.top) * scale, powers);
+            if (!end) goal = fmax(goal, least);
+        }
+        const bool ends = chunks > 1 && __any(end && least > 0.0);
         // the block (four draws' sums requested at a time)
         int32_t block = 0;
         for (int32_t t4 = 0; t4 < many; t4 += 4) {
@@ -882,7 +890,7 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
         const double *of_quarter = sums + (int64_t)chunk * kSums + kBlocks;
         int32_t quarter = kQuarters - 1;
         if (end) {
-            while (quarter > 0 && !(of_quarter[quarter] > 0.0)) --quarter;
+            while (quarter > 0 && !(of_quarter[quarter] > least)) --quarter;
             goal = __builtin_inf();
         } else {
             const double2 a = reinterpret_cast<const double2 *>(of_quarter)[2 * block];
@@ -934,7 +942,12 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
                 const double upto = row_prefix(weight);
                 const u64 positive = __ballot(weight > 0.0), past = __ballot(upto > g) & positive;
                 const uint32_t in_row = (uint32_t)(past >> (lane & 48)) & 0xFFFFu;
-                const uint32_t have = (uint32_t)(positive >> (lane & 48)) & 0xFFFFu;
+                uint32_t have = (uint32_t)(positive >> (lane & 48)) & 0xFFFFu;
+                if (ends) {  // (a goal past all: the last with weight beside the row's largest)
+                    const u64 above = __ballot(weight > __shfl(least, t));
+                    const uint32_t its = (uint32_t)(above >> (lane & 48)) & 0xFFFFu;
+                    have = its && !(g < __builtin_inf()) ? its : have;
+                }
                 const int l = in_row ? __builtin_ctz(in_row) : 31 - __builtin_clz(have | 1u);
                 if (place == l && t < many) {
                     word[d0 + t0 + t] = base[j] + place;

@@ -1050,3 +1050,21 @@ def test_pack_every_power_of_two(state):
         np.testing.assert_array_equal(out.e.cpu().numpy(), e)
         np.testing.assert_array_equal(ow.value8(out.q.view(torch.uint8).cpu().numpy()),
                                       ow.value8(q))
+
+
+@pytest.mark.parametrize("V,temperature", [(20000, 0.01), (20000, 1e-3), (70000, 0.004),
+                                           (600000, 0.003), (5000, 0.01)])
+def test_draw_ends_at_low_temperatures(state, V, temperature):
+    """Uniforms at the ends draw the first and the last word with weight, where most words'
+    weights are below the least fp64 value, beside the row's largest if not their chunk's."""
+    say(f"draw: ends of {V} words at {temperature}")
+    rng = np.random.default_rng(V)
+    x = _scores(rng, 6, V, torch.float32)
+    x[3:] *= 0.5
+    u = np.tile(np.array([0.0, -1.0, 1.0, np.nan, 0.37, 0.99]), (6, 1))
+    for r in (None, RuleSet(rng, 6, V, listed=False)):
+        word, logp = _outs(6, 6)
+        sp.spdp_draw(state.h, x, word, logp, work_for(6, V), u=dev(u), rules=r and r.c,
+                     temperature=temperature)
+        xo = x.cpu().numpy() if r is None else r.oracle(x)
+        _check_draws(word.cpu().numpy(), logp.cpu().numpy(), xo, u, temperature, most_skipped=0.2)
