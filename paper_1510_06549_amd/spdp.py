@@ -528,6 +528,7 @@ class _Device:
     def _hip(name, *args):
         rc = getattr(lib(), name)(*args)
         if rc:
+            lib().hipGetLastError()  # (else it is the error of the next launch)
             raise SpdpError(SPDP_E_HIP, f"{name}: HIP error {rc}")
 
     @classmethod

@@ -1068,3 +1068,12 @@ def test_draw_ends_at_low_temperatures(state, V, temperature):
                      temperature=temperature)
         xo = x.cpu().numpy() if r is None else r.oracle(x)
         _check_draws(word.cpu().numpy(), logp.cpu().numpy(), xo, u, temperature, most_skipped=0.2)
+
+
+def test_calls_after_a_failed_allocation(state):
+    """What an allocation that failed leaves behind is no error of the next call."""
+    say("calls after an allocation that failed")
+    with pytest.raises(sp.SpdpError):
+        sp._Device((1 << 50,), "uint8")
+    out = sp.spdp_pack8(state.h, torch.ones((2, 3), device="cuda"), sp.Rows8.empty(2, 3))
+    assert (out.q[:, :3].float() == 256).all()
