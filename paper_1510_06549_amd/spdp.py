@@ -874,6 +874,8 @@ class Sampler:
         theta, phi = np.asarray(theta, np.float64), np.asarray(phi, np.float64)
         if theta.ndim != 2 or phi.ndim != 2 or theta.shape[1] != phi.shape[1]:
             raise ValueError("theta [D, K] and phi [V, K]")
+        if top < 0 or draws < 0:
+            raise ValueError("top and draws: how many words of each document")
         D, V = len(theta), len(phi)
 
         def put(x, dtype):

@@ -185,3 +185,14 @@ def test_product8_without_words(type, ld, text):
         STATE, C.addressof(none), C.addressof(none), 0, P, *a)
     refused(call(type, ld), text)
     assert call(sp.SPDP_F16, 0) == sp.SPDP_OK
+
+
+def test_binding_predict_wants_counts():
+    import numpy as np
+
+    s = object.__new__(sp.Sampler)
+    s.h = None
+    for kw in (dict(top=-1), dict(draws=-1), dict(top=5, draws=-2)):
+        for rows in (0, 2):
+            with pytest.raises(ValueError, match="how many words"):
+                s.predict(np.ones((rows, 3)), np.ones((5, 3)), **kw)
