@@ -889,8 +889,11 @@ class Sampler:
                 if len(doc_words) != D:
                     raise ValueError("doc_words: one list per document")
                 r["doc_off"] = put(np.cumsum([0] + [len(w) for w in doc_words]), "int64")
-                r["words"] = put(np.concatenate([np.asarray(w, np.int32) for w in doc_words] +
-                                                [np.empty(0, np.int32)]), "int32")
+                w = np.concatenate([np.asarray(w, np.int64) for w in doc_words] +
+                                   [np.empty(0, np.int64)])
+                # (words that are none of the vocabulary's are ignored, those too that 32 bits
+                # would turn into some)
+                r["words"] = put(np.where((w >= 0) & (w < V), w, -1), "int32")
                 r["penalties"] = put(np.broadcast_to(np.asarray(penalties, np.float32), (D, 3)),
                                      "float32")
             if bias is not None:

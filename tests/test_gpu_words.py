@@ -1077,3 +1077,14 @@ def test_calls_after_a_failed_allocation(state):
         sp._Device((1 << 50,), "uint8")
     out = sp.spdp_pack8(state.h, torch.ones((2, 3), device="cuda"), sp.Rows8.empty(2, 3))
     assert (out.q[:, :3].float() == 256).all()
+
+
+def test_predict_words_beyond_32_bits(state):
+    """Listed words that are none of the vocabulary's are ignored, however large."""
+    say("predict: listed words beyond 32 bits")
+    theta, phi = np.ones((2, 3)), np.arange(1, 31).reshape(10, 3) / 32.0
+    plain = state.predict(theta, phi, top=4)[:2]
+    odd = [np.array([2 ** 32 + 9, -1, 2 ** 40, 10]), [2 ** 33 + 8, -2 ** 31 - 1 + 9]]
+    got = state.predict(theta, phi, top=4, doc_words=odd, penalties=(1.0, 1e9, 0.0))[:2]
+    for a, b in zip(got, plain):
+        np.testing.assert_array_equal(a, b)
