@@ -7,6 +7,7 @@ this module raises if ``libspdp.so`` has not been built.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -532,6 +533,23 @@ class _Device:
             raise SpdpError(SPDP_E_HIP, f"{name}: HIP error {rc}")
 
     @classmethod
+    def current(cls):
+        d = C.c_int()
+        cls._hip("hipGetDevice", C.byref(d))
+        return d.value
+
+    @classmethod
+    @contextlib.contextmanager
+    def on(cls, device):
+        """Memory and waits are of this device inside; the caller's is current again after."""
+        before = cls.current()
+        cls._hip("hipSetDevice", C.c_int(device))
+        try:
+            yield
+        finally:
+            cls._hip("hipSetDevice", C.c_int(before))
+
+    @classmethod
     def wait(cls):
         cls._hip("hipDeviceSynchronize")
 
@@ -747,6 +765,7 @@ class Sampler:
             self.h = spdp_create_assoc(words, doc_offsets, doc_group, n_groups, vocab, K, alpha,
                                        a, b, gamma, row_off, src, p, init_seed=init_seed,
                                        hip_stream=hip_stream)
+        self.device = _Device.current()  # (the state's: it is made on the current one)
         self.info = spdp_info(self.h)
         self.N, self.G, self.V, self.K = (self.info["N"], self.info["G"], self.info["V"],
                                           self.info["K"])
@@ -877,7 +896,12 @@ class Sampler:
         if top < 0 or draws < 0:
             raise ValueError("top and draws: how many words of each document")
         D, V = len(theta), len(phi)
+        with _Device.on(self.device):
+            return self._predict(theta, phi, D, V, top, draws, seed, step, temperature, doc_words,
+                                 penalties, bias, allowed)
 
+    def _predict(self, theta, phi, D, V, top, draws, seed, step, temperature, doc_words, penalties,
+                 bias, allowed):
         def put(x, dtype):
             x = np.asarray(x, dtype)
             return _Device(x.shape, dtype, x)

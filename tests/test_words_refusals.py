@@ -196,3 +196,57 @@ def test_binding_predict_wants_counts():
         for rows in (0, 2):
             with pytest.raises(ValueError, match="how many words"):
                 s.predict(np.ones((rows, 3)), np.ones((5, 3)), **kw)
+
+
+class TwoDevices:
+    """What Sampler.predict asks of the library, with the device that is current recorded: the
+    state's is 1."""
+
+    def __init__(self, error=0):
+        self.device, self.error, self.mine, self.elsewhere, self.at = 0, error, 0, [], 1 << 20
+
+    def __getattr__(self, name):
+        def call(*args):
+            if self.device == 1:
+                self.mine += 1
+            else:
+                self.elsewhere.append(name)
+            if name == "hipMalloc":
+                self.at += 1 << 20
+                args[0]._obj.value = self.at
+            elif name == "spdp_predict_work":
+                args[-1]._obj.value = 64
+            elif name == "spdp_predict":
+                return self.error
+            elif name == "spdp_last_error":
+                return b"refused"
+            return 0
+
+        return call
+
+    def hipGetDevice(self, out):
+        out._obj.value = self.device
+        return 0
+
+    def hipSetDevice(self, device):
+        self.device = device.value
+        return 0
+
+
+@pytest.mark.parametrize("error", [0, sp.SPDP_E_ARG])
+def test_binding_predict_on_the_states_device(monkeypatch, error):
+    """Memory comes from the device that the state was made on, whichever is current."""
+    import numpy as np
+
+    lib = TwoDevices(error)
+    monkeypatch.setattr(sp, "lib", lambda: lib)
+    s = object.__new__(sp.Sampler)
+    s.h, s.device = None, 1
+    call = lambda: s.predict(np.ones((2, 3)), np.ones((5, 3)), top=2, draws=1)  # noqa: E731
+    if error:
+        with pytest.raises(sp.SpdpError, match="refused"):
+            call()
+    else:
+        assert [x.shape for x in call()] == [(2, 2), (2, 2), (2, 1), (2, 1)]
+    assert lib.device == 0 and lib.mine > 10
+    assert set(lib.elsewhere) <= {"hipFree"}
