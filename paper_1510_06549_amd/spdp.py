@@ -924,7 +924,7 @@ class Sampler:
                 r["bias"] = put(np.reshape(bias, (1, V)), "float32")
             if allowed is not None:
                 bits = np.zeros(-(-V // 32) * 32, np.uint8)
-                bits[:V] = np.asarray(allowed, bool)
+                bits[:V] = np.reshape(allowed, V).astype(bool)
                 r["mask"] = put(np.packbits(bits, bitorder="little").view("<i4")[None], "int32")
             rules = Rules(D, V, **r)
         packed = []

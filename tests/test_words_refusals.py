@@ -250,3 +250,18 @@ def test_binding_predict_on_the_states_device(monkeypatch, error):
         assert [x.shape for x in call()] == [(2, 2), (2, 2), (2, 1), (2, 1)]
     assert lib.device == 0 and lib.mine > 10
     assert set(lib.elsewhere) <= {"hipFree"}
+
+
+@pytest.mark.parametrize("kw", [dict(allowed=True), dict(allowed=[True]), dict(allowed=[True] * 4),
+                                dict(allowed=[[True] * 5] * 2), dict(bias=[0.5])])
+def test_binding_predict_wants_whole_tables(monkeypatch, kw):
+    """One truth value is not one for every word."""
+    import numpy as np
+
+    lib = TwoDevices()
+    monkeypatch.setattr(sp, "lib", lambda: lib)
+    s = object.__new__(sp.Sampler)
+    s.h, s.device = None, 1
+    with pytest.raises(ValueError, match="reshape"):
+        s.predict(np.ones((2, 3)), np.ones((5, 3)), top=2, **kw)
+    s.predict(np.ones((2, 3)), np.ones((5, 3)), top=2, allowed=[1, 0, 1, 0, 1], bias=range(5))
