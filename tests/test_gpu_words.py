@@ -1088,3 +1088,134 @@ def test_predict_words_beyond_32_bits(state):
     got = state.predict(theta, phi, top=4, doc_words=odd, penalties=(1.0, 1e9, 0.0))[:2]
     for a, b in zip(got, plain):
         np.testing.assert_array_equal(a, b)
+
+
+# ---------------------------------------------------------------------------
+# products of every shape of workgroup
+# ---------------------------------------------------------------------------
+def _model8(state, seed, m, n, cols):
+    """Packed theta- and phi-like rows (positive, zeros among them, scales far apart) and their
+    values in fp64, on the device."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    sides = []
+    for rows, spread in ((m, 2.0), (n, 3.0)):
+        x = torch.randn((rows, cols), device="cuda", generator=gen).mul_(spread).exp_()
+        x[torch.rand((rows, cols), device="cuda", generator=gen) < 0.05] = 0
+        x *= torch.randn((rows, 1), device="cuda", generator=gen).mul_(2).exp_()
+        p = sp.spdp_pack8(state.h, x, sp.Rows8.empty(rows, cols))
+        nb = p.e.shape[1]
+        v = p.q.double().view(rows, nb, 128) * torch.exp2(p.e.double() - 127)[:, :, None]
+        sides.append((p, v.view(rows, nb * 128)))
+    return sides
+
+
+def _all_products(state, m, n, cols, type, log, ld):
+    """Every output within the sums' tolerance, and rows equal to those of batches of 16
+    (which a kernel of their own makes)."""
+    (a8, a), (b8, b) = _model8(state, m + n + cols, m, n, cols)
+    dtype = TYPES[type]
+    out, buf = framed(m, n, dtype, ld=ld, fill=-3.0)
+    sp.spdp_product8(state.h, a8, b8, out, log=log)
+    assert frame_kept(buf, out, -3.0)
+    del buf
+    # (sums of positive values: off by P 2^-23 of themselves at most)
+    rel = a.shape[1] * 2.0 ** -23
+    half = torch.finfo(dtype).eps / 2
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    step = max(1, 50000000 // n)
+    bt = b.T.contiguous()
+    for i in range(0, m, step):
+        ref = a[i:i + step] @ bt
+        if log:
+            want = ref.log()
+            tol = 1.01 * rel + 2.0 ** -22 * (want.abs() + 1)
+        else:
+            want, tol = ref, rel * ref
+        got = out[i:i + step].double()
+        tol = (tol + half * want.abs() + tiny) * (1 + half)
+        bad = ~((got - want).abs() <= tol)
+        assert not bad.any(), (i, bad.nonzero()[:5].tolist())
+    few = torch.empty((16, n), dtype=dtype, device="cuda")
+    for i in sorted({0, m // 2, m - 16}):
+        part = sp.Rows8(a8.q[i:i + 16], a8.e[i:i + 16], cols)
+        assert torch.equal(sp.spdp_product8(state.h, part, b8, few, log=log), out[i:i + 16]), i
+
+
+# Documents a workgroup takes by its own rule (16 for each fragment), rounds of words of a
+# wavefront, and blocks of columns: all columns at once in LDS up to 32 / fragments of them, and
+# part by part beyond.  Outputs above 64 MB whose rows start at multiples of 64 bytes are streamed.
+PRODUCTS = [
+    # m, n, cols, type, log, ld
+    (200, 14724, 300, "f32", True, 14724),     # 2 fragments, 3 blocks
+    (9000, 2048, 129, "f32", False, 2048),     # streamed, 2 blocks
+    (65, 4100, 2100, "f32", True, 4100),       # 2, 17 blocks: two parts
+    (300, 50000, 129, "f32", True, 50000),     # 4, 2 rounds, 2 blocks
+    (300, 100016, 500, "f32", True, 100016),   # 4, 4 rounds, 4 blocks, streamed
+    (300, 100001, 500, "bf16", True, 100007),  # 4, odd pitch
+    (300, 50000, 1100, "bf16", True, 50000),   # 4, 9 blocks: two parts in each of 2 rounds
+    (400, 100016, 300, "bf16", True, 100032),  # 6, 4 rounds, 3 blocks, streamed
+    (777, 20000, 640, "f32", False, 20001),    # 6, 2 rounds, 5 blocks: the LDS full
+    (777, 20011, 700, "f32", True, 20011),     # 6, 2 rounds, 6 blocks: two parts
+    (2000, 10000, 1000, "f32", True, 10000),   # 6, streamed, two parts
+    (777, 14724, 64, "f32", False, 14724),     # 8, 1 round
+    (500, 50000, 500, "bf16", True, 50000),    # 8, 2 rounds, 4 blocks: the LDS full
+    (1000, 50000, 513, "bf16", True, 50016),   # 8, 4 rounds, 5 blocks: two parts, streamed
+    (1500, 20001, 1000, "f32", False, 20001),  # 8, 2 rounds, 8 blocks: two parts
+    (97, 100016, 1500, "f32", True, 100016),   # 8, 12 blocks: three parts
+    (2000, 100000, 500, "bf16", True, 100000),  # 8, 13 rounds, 4 blocks, streamed
+    (1000, 100000, 200, "f32", False, 100000),  # 8, 7 rounds, streamed
+]
+
+
+@pytest.mark.parametrize("m,n,cols,type,log,ld", PRODUCTS)
+def test_products_of_large_batches(state, m, n, cols, type, log, ld):
+    say(f"product {m} x {n} x {cols} {type} log={log}, rows {ld} apart")
+    _all_products(state, m, n, cols, type, log, ld)
+
+
+@pytest.mark.parametrize("m,n,cols,ld", [(1, 5000, 50, 5000), (16, 1000, 300, 1003),
+                                         (50, 3000, 500, 3001), (777, 14724, 64, 14724),
+                                         (1000, 40000, 64, 40000)])
+def test_product_of_probabilities_in_fp16(state, m, n, cols, ld):
+    """Rows that add up to 1 against values up to 1: sums that fp16 holds."""
+    say(f"probabilities {m} x {n} x {cols} in fp16")
+    rng = np.random.default_rng(m + n)
+    theta = rng.dirichlet(np.full(cols, 0.1), size=m)
+    phi = rng.random((n, cols)) ** 8
+    sides = [sp.spdp_pack8(state.h, dev(x), sp.Rows8.empty(*x.shape)) for x in (theta, phi)]
+    a, b = (ow.unpack8(p.q.view(torch.uint8).cpu().numpy(), p.e.cpu().numpy()) for p in sides)
+    out, buf = framed(m, n, torch.float16, ld=ld)
+    sp.spdp_product8(state.h, *sides, out)
+    some = np.unique(np.r_[0:min(m, 40), max(0, m - 40):m])
+    _check_product(out[dev(some)].double().cpu().numpy(), a[some], b, False, torch.float16)
+    assert frame_kept(buf, out)
+
+
+@pytest.mark.parametrize("n", [2, 66])
+def test_every_scale(state, n):
+    """Every positive value at every scale times powers of two that bring it into fp32's
+    range: itself for scales of 2^-124 to 2^119, rounded to bf16 beyond."""
+    say(f"product, every scale, {n} words")
+    e, code = np.meshgrid(np.arange(255), np.arange(127), indexing="ij")
+    e, code = e.ravel(), code.ravel()
+    q = np.zeros((len(e), 128), np.uint8)
+    q[:, 0] = code
+    a8 = sp.Rows8(dev(q).view(torch.float8_e4m3fn), dev(e[:, None].astype(np.uint8)), 1)
+    value = np.ldexp(ow.VALUES8[code], e - 127)  # (fp64)
+    # 8 bits of fraction at a time, and the steps of 2^-133 below bf16's normal range
+    step = np.ldexp(1.0, np.maximum(np.frexp(value)[1] - 8, -133))
+    rounded = np.rint(value / step) * step
+    rounded[rounded >= 2.0 ** 128] = np.inf
+    exact = (e >= 3) & (e <= 246)
+    assert np.array_equal(rounded[exact], value[exact])
+    power = np.where(np.arange(n) % 2 == 0, 100, -100)
+    qb = np.zeros((n, 128), np.uint8)
+    qb[:, 0] = 0x38  # 1
+    b8 = sp.Rows8(dev(qb).view(torch.float8_e4m3fn), dev((power + 127)[:, None].astype(np.uint8)), 1)
+    got = sp.spdp_product8(state.h, a8, b8, torch.empty((len(e), n), device="cuda")).cpu().numpy()
+    for j in range(n):
+        want = rounded * 2.0 ** power[j]
+        want[want >= 2.0 ** 128] = np.inf
+        normal = (want == 0) | (want >= 2.0 ** -126)  # (what a sum below fp32's range is, is its own)
+        bad = normal & (got[:, j].astype(np.float64) != want)
+        assert not bad.any(), (j, [(e[i], code[i], got[i, j], want[i]) for i in np.flatnonzero(bad)[:5]])
