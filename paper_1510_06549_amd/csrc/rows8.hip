@@ -68,19 +68,19 @@ __device__ __forceinline__ int max32(int v)
 // bits.  Bound by the read: 100 000 rows of 500 doubles (400 MB, 52 written) take 79 us (5.7
 // TB/s), of floats 58 us in twos (4.3 TB/s).
 template <typename T, int UNITS>
-__global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, int64_t units,
+__global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, uint32_t units,
                                                int32_t cols, int64_t ld, int32_t nb,
                                                uint8_t *__restrict__ q, uint8_t *__restrict__ e)
 {
     typedef T quad __attribute__((ext_vector_type(4), aligned(4)));
-    const int64_t first = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * UNITS;
+    const uint32_t first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * UNITS;
     const int lane = threadIdx.x & 31;
     double v[UNITS][4];
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
-        const int64_t unit = first + i < units ? first + i : units - 1;
-        const int64_t row = units <= UINT32_MAX ? (uint32_t)unit / (uint32_t)nb : unit / nb;
-        const int32_t c = (int32_t)(unit - row * nb) * kBlock + 4 * lane;
+        const uint32_t unit = first + i < units ? first + i : units - 1;
+        const uint32_t row = unit / (uint32_t)nb;
+        const int32_t c = (int32_t)(unit - row * (uint32_t)nb) * kBlock + 4 * lane;
         const T *src = x + row * ld + c;
         if (c + 4 <= cols) {
             const quad a = *reinterpret_cast<const quad *>(src);
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, int64_t 
         word = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_odd(v[i][2], ex), scaled_odd(v[i][3], ex),
                                                word, true);
         if (first + i < units) {
-            *reinterpret_cast<int *>(q + (first + i) * kBlock + 4 * lane) = word;
+            *reinterpret_cast<int *>(q + (int64_t)(first + i) * kBlock + 4 * lane) = word;
             if (lane == 0) e[first + i] = (uint8_t)(ex + 127);
         }
     }
@@ -553,11 +553,12 @@ hipError_t launch_pack8(const void *x, int32_t type, int64_t rows, int32_t cols,
 {
     const int32_t nb = blocks8(cols);
     if (rows == 0 || nb == 0) return hipSuccess;
-    const int64_t step = kLaunchBlocks / nb * 8;  // (rows of a launch; nb is at most 2^17)
+    // rows of a launch: nb is at most 2^17, and units stay below 8 kLaunchBlocks < 2^26
+    const int64_t step = kLaunchBlocks / nb * 8;
     for (int64_t row = 0; row < rows; row += step) {
-        const int64_t units = (rows - row < step ? rows - row : step) * nb;
-        const auto blocks = [&](int per) {
-            return dim3((unsigned)((units + 8 * per - 1) / (8 * per)));
+        const uint32_t units = (uint32_t)((rows - row < step ? rows - row : step) * nb);
+        const auto blocks = [&](uint32_t per) {
+            return dim3((units + 8 * per - 1) / (8 * per));
         };
         uint8_t *to = q + row * nb * kBlock, *scales = e + row * nb;
         if (type == SPDP_F64)
