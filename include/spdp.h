@@ -313,10 +313,12 @@ int spdp_align_topics(const double *h, int32_t kp, int32_t kq, int32_t *match, d
  * state's counts are neither read nor changed), take device pointers only, allocate
  * nothing and do not synchronise: they can be captured into a HIP graph.
  * Buffers are checked to be memory of the state's device that holds their size
- * (against the device allocation, not against a caller's sub-range of it), aligned to
+ * (against the device allocation, not against a caller's sub-range of it; host memory that
+ * is pinned, and so has an address on the device, passes), aligned to
  * their elements; what they hold is not checked on the host, and each entry point says
- * what becomes of values out of range.  A workspace belongs to one call at a time: calls that overlap
- * (other streams, other graphs) need workspaces of their own.
+ * what becomes of values out of range.  Outputs and workspaces share no memory with inputs
+ * or with each other, except where an entry point allows it.  A workspace belongs to one
+ * call at a time: calls that overlap (other streams, other graphs) need workspaces of their own.
  */
 
 /* Types of values in device memory. */
@@ -331,7 +333,8 @@ int spdp_align_topics(const double *h, int32_t kp, int32_t kq, int32_t *match, d
 /*
  * Rows in 8-bit floating point (e4m3: largest value 448, no infinities), with a
  * power of two as the scale of each block of SPDP_BLOCK8 columns of a row:
- * element (i, k) is q[i][k] 2^(e[i][k / SPDP_BLOCK8] - 127).
+ * element (i, k) is q[i][k] 2^(e[i][k / SPDP_BLOCK8] - 127).  An e of 255 makes its block's
+ * elements NaN.
  */
 typedef struct {
     int64_t rows;               /* 0 <= rows < 2^31                                   */
@@ -435,8 +438,8 @@ int spdp_top(spdp_state *s, const void *x, int64_t ld, int32_t type, int64_t row
  * - max x') / temperature): the first word whose prefix sum of the weights exceeds
  * u times their sum, in fp64.  word [rows][draws] int32 and logp [rows][draws]
  * fp32, the logarithm of the drawn word's probability (device).  u is device
- * [rows][draws] fp64 (0 and less draw the first word with positive weight; 1 and
- * more, and NaN, the last); NULL takes the uniforms x0 2^-32 of Philox4x32-10
+ * [rows][draws] fp64 (0 and less draw the first word with positive weight, that is with one
+ * that fp64 does not round to 0; 1 and more, and NaN, the last); NULL takes the uniforms x0 2^-32 of Philox4x32-10
  * keyed by `seed` at counter (row draws + draw, step) with purpose 4 (first word).
  * A row without a law (every score -inf; NaN or +inf among them) gives word -1 and
  * logp NaN.

@@ -65,8 +65,8 @@ __device__ __forceinline__ int max32(int v)
 
 // Half a wavefront per (row, block), four columns a lane, UNITS blocks whose columns are all
 // requested first; whole numbers throughout, as the scale is an exponent and the rounding
-// bits.  Bound by the read: 100 000 rows of 500 doubles (400 MB, 52 written) take 79 us (5.7
-// TB/s), of floats 58 us in twos (4.3 TB/s).
+// bits.  Bound by the read: 100 000 rows of 500 doubles (400 MB, 52 written) take 78 us (5.8
+// TB/s), of floats 55 us in twos (4.6 TB/s).
 template <typename T, int UNITS>
 __global__ void __launch_bounds__(256) k_pack8(const T *__restrict__ x, uint32_t units,
                                                int32_t cols, int64_t ld, int32_t nb,
@@ -207,7 +207,7 @@ __device__ __forceinline__ void store_unit(T *p, i4v v)
 // Columns past kLdsBlocks / FD blocks do not fit the LDS at once: then documents are
 // staged again, part by part, for every round of words.
 //
-// 2 000 x 100 000 x 500 (512 padded) to logarithms in bf16: 179 us, 1 140 TFLOP/s of the
+// 2 000 x 100 000 x 500 (512 padded) to logarithms in bf16: 180 us, 1 140 TFLOP/s of the
 // padded products; 137 us without stores and logarithms, where a large product of the library
 // takes 140 at its best rate (1 430 TFLOP/s at 8 192 cubed, and 404 us for these sizes).  The
 // stores, 400 MB, and the logarithms run under other wavefronts' products only in part.
@@ -462,7 +462,8 @@ __global__ void __launch_bounds__(256) k_product8_few(
 // tile's words, the rounds of words that each of their wavefronts takes, and what that
 // costs.  A compute unit takes `turns` workgroups one after another; a round takes as long
 // as its products or 3 more document fragments' (its words' conversion and stores), a
-// workgroup's start as long as 2 of them.
+// workgroup's start as long as 2 of them.  (What it costs to stage documents part by part, past
+// kLdsBlocks / fd blocks of columns, is not counted.)
 struct Shares {
     int64_t tiles_d, ranges, rounds, cost;
 };
@@ -481,13 +482,14 @@ Shares shares_of(int64_t m, int64_t n, int32_t fd, int64_t turns)
 }
 
 // Scores above kStreamBytes are written past the caches' usual order: they would push out
-// the words, which every tile of documents reads again (2 000 x 100 000 in bf16, 400 MB: 237
-// us, 192 streamed; 1 000 x 100 000 of 64 topics in fp16, 200 MB: 72 and 56 us).  Less than
-// that stays in the last level cache for whoever reads it next, and takes less time too (777
-// x 14 724 in fp16, 23 MB: 11.2 us, 15.0 streamed).  Rows have to start at multiples of 64
-// bytes: lines that are written in parts are not put together past the caches (2 000 x 99 999
-// of 500 topics in bf16: 384 us streamed, 272 not; 2 000 x 100 016, rows at multiples of 32
-// bytes: 256 and 233, of 700 topics 296 and 340).
+// the words, which every tile of documents reads again (2 000 x 100 000 of 500 topics: in bf16,
+// 400 MB, 180 us streamed, 230 not; in fp32 218 and 270; 1 000 x 100 000 of 64 topics in fp16,
+// 200 MB, 57 streamed, 70 not).  Less than that stays in the last level cache for whoever reads
+// it next, and takes less time too (777 x 14 724 of 64 topics in fp16, 23 MB: 12.9 us streamed,
+// 11.0 not).  Rows have to start at multiples of 64 bytes: lines that are written in parts are
+// not put together past the caches (2 000 x 99 999 of 500 topics in bf16: 388 us streamed, 274
+// not; 2 000 x 100 016, rows at multiples of 32 bytes: 257 streamed, 233 not; of 700 topics,
+// where more work hides the stores, 301 streamed, 340 not).
 template <typename T, bool LOG, int FD, bool STREAM>
 hipError_t product(const spdp_rows8 &a, const spdp_rows8 &b, void *c, int64_t ld, const Shares &s,
                    hipStream_t st)

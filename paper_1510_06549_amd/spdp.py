@@ -887,7 +887,10 @@ class Sampler:
                 doc_words=None, penalties=(1.0, 0.0, 0.0), bias=None, allowed=None):
         """Words for documents from host estimates theta [D, K] and phi [V, K] (a group's, or
         phi0): (top words [D, top], their scores, drawn words [D, draws], their log
-        probabilities).  doc_words: a list of word ids for every document, which `penalties`
+        probabilities).  Both are rounded to 8 bits with a scale for each 128 topics (spdp_pack8:
+        a value is off by 2^-4 of itself at most, or 2^-10 of its scale), so that words whose scores
+        are closer than that may change places; both are packed anew by every call, and a program
+        that asks often keeps Rows8 of its own and calls spdp_predict.  doc_words: a list of word ids for every document, which `penalties`
         = (repeat, presence, frequency) make less likely; bias [V]: added to the scores;
         allowed [V]: truth values, the words to choose from."""
         theta, phi = np.asarray(theta, np.float64), np.asarray(phi, np.float64)

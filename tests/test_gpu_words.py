@@ -1219,3 +1219,18 @@ def test_every_scale(state, n):
         normal = (want == 0) | (want >= 2.0 ** -126)  # (what a sum below fp32's range is, is its own)
         bad = normal & (got[:, j].astype(np.float64) != want)
         assert not bad.any(), (j, [(e[i], code[i], got[i, j], want[i]) for i in np.flatnonzero(bad)[:5]])
+
+
+@pytest.mark.parametrize("n", [2, 66])
+def test_scale_that_is_none(state, n):
+    say(f"product, scale byte 255, {n} words")
+    q = np.zeros((127, 256), np.uint8)
+    q[:, 0], q[:, 1], q[:, 130] = np.arange(127), 0x38, 0x38
+    e = np.full((127, 2), 127, np.uint8)
+    e[:60, 0] = 255
+    qb = np.zeros((n, 256), np.uint8)
+    qb[:, 130] = 0x38
+    a8, b8 = (sp.Rows8(dev(q).view(torch.float8_e4m3fn), dev(e), 200),
+              sp.Rows8(dev(qb).view(torch.float8_e4m3fn), dev(np.full((n, 2), 127, np.uint8)), 200))
+    got = sp.spdp_product8(state.h, a8, b8, torch.empty((127, n), device="cuda"))
+    assert torch.isnan(got[:60]).all() and (got[60:] == 1).all()
