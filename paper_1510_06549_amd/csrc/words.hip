@@ -646,7 +646,9 @@ __device__ __forceinline__ double lane_before(double v)  // (0 for the first)
 __device__ __forceinline__ void rising(const double (&share)[2], double (&upto)[2])
 {
     const double all = prefix(share[0] + share[1]);
-    const double a = share[0] > 0.0 ? lane_before(all) + share[0] : 0.0;
+    // (all lanes hand theirs on: one that a branch leaves out would give 0)
+    const double to_here = lane_before(all);
+    const double a = share[0] > 0.0 ? to_here + share[0] : 0.0;
     const double b = share[1] > 0.0 ? all : 0.0;
     const double before = lane_before(largest_upto(fmax(a, b)));
     upto[0] = fmax(before, a);

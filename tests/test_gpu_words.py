@@ -1234,3 +1234,30 @@ def test_scale_that_is_none(state, n):
               sp.Rows8(dev(qb).view(torch.float8_e4m3fn), dev(np.full((n, 2), 127, np.uint8)), 200))
     got = sp.spdp_product8(state.h, a8, b8, torch.empty((127, n), device="cuda"))
     assert torch.isnan(got[:60]).all() and (got[60:] == 1).all()
+
+
+@pytest.mark.parametrize("V", [100, 5000, 9000, 30000, 700000])
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+def test_draw_from_few_words(state, V, type):
+    """Rows of which a mask, or scores of -inf, leave a few words here and there: most sums of
+    16, 64 and 8 192 words are 0."""
+    say(f"draw: few words of {V} {type}")
+    rng = np.random.default_rng(V)
+    rows, n = 10, 200 if V <= 30000 else 24
+    x = _scores(rng, rows, V, TYPES[type])
+    keep = np.zeros((rows, V), bool)
+    for i, many in enumerate([1, 2, 3, 4, 5, 8, 20, 50, 100, 300]):
+        keep[i, rng.integers(0, V, many)] = True
+    keep[1, [V // 2, V // 2 + 1]] = True  # (neighbours, and both ends)
+    keep[2, [0, V - 1]] = True
+    bits = np.zeros((rows, -(-V // 32) * 32), np.uint8)
+    bits[:, :V] = keep
+    r = sp.Rules(rows, V, mask=dev(np.packbits(bits, axis=1, bitorder="little").view("<i4").copy()),
+                 mask_of=dev(np.arange(rows, dtype=np.int32)))
+    u = rng.random((rows, n))
+    xo = np.where(keep, x.float().cpu().numpy(), -np.inf).astype(np.float32)
+    for scores, rules in ((x, r), (dev(xo, TYPES[type]), None)):
+        for uniforms in (u, np.where(np.arange(n) % 3 == 1, 1.0, u)):
+            word, logp = _outs(rows, n)
+            sp.spdp_draw(state.h, scores, word, logp, work_for(rows, V), u=dev(uniforms), rules=rules)
+            _check_draws(word.cpu().numpy(), logp.cpu().numpy(), xo, uniforms, 1.0)
