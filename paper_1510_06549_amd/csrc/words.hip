@@ -838,9 +838,9 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
             const double sum = of_lane(law.upto, 63);
             const bool last = c0 >= law.last;
             const u64 some = __ballot(law.some);
-            const int at = chunks == 1 ? 0
-                           : end       ? 63 - __builtin_clzll(some | 1)
-                                       : first_past(law.upto, sum, goal);
+            // (by all lanes: draws at the end hand their chunks' sums to the others)
+            const int past = chunks == 1 ? 0 : first_past(law.upto, sum, goal);
+            const int at = chunks > 1 && end ? 63 - __builtin_clzll(some | 1) : past;
             const double before = __shfl(law.upto, at ? at - 1 : 0);
             const double its = __shfl(law.own, at), inverse = __shfl(law.inverse, at);
             if (!found && (last || (!end && sum > goal))) {
