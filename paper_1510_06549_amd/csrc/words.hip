@@ -673,7 +673,7 @@ __device__ __forceinline__ int first_past(double upto, double last, double goal)
 struct Law {
     double top, total;    // largest score; sum of the weights
     double upto;          // sum of the weights up to and with this lane's chunk;
-    double own, inverse;  // its largest score, and by what its own weights exceed theirs
+    double own, inverse;  // its largest score, and 2^-100 of what its own weights are times theirs
     bool some;            // whether it holds some weight
     int32_t last;         // first of the last 64 chunks that hold some weight
     bool is;
@@ -685,14 +685,14 @@ __device__ __forceinline__ void lane_chunk(Law &law, const Part *part, int32_t c
 {
     double share = 0.0;
     law.own = law.top;
-    law.inverse = 1.0;
+    law.inverse = 0x1p-100;
     if (c < chunks) {
         const Part p = part[c];
         if (p.sum > 0.0) {
             const double w = power_of((p.top - law.top) * scale, powers);
             share = p.sum * w;
             law.own = p.top;
-            law.inverse = 1.0 / w;
+            law.inverse = 1.0 / (w * 0x1p+100);  // (finite for the least weights)
         }
     }
     law.some = share > 0.0;
@@ -848,7 +848,7 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
                 chunk = min(c0 + at, chunks - 1);
                 own = its;
                 goal = at ? goal - before : goal;
-                goal = goal > 0.0 ? goal * inverse : 0.0;
+                goal = goal > 0.0 ? goal * 0x1p+100 * inverse : 0.0;
             } else if (!found) {
                 goal -= sum;
             }

@@ -1261,3 +1261,23 @@ def test_draw_from_few_words(state, V, type):
             word, logp = _outs(rows, n)
             sp.spdp_draw(state.h, scores, word, logp, work_for(rows, V), u=dev(uniforms), rules=rules)
             _check_draws(word.cpu().numpy(), logp.cpu().numpy(), xo, uniforms, 1.0)
+
+
+@pytest.mark.parametrize("at", [-690.0, -705.0, -709.0, -720.0, -735.0])
+def test_draw_among_the_least_weights(state, at):
+    """Uniforms among weights near and below fp64's normal range, in a chunk of words that hold
+    no others."""
+    say(f"draw: words of weight exp({at})")
+    V = 20000
+    x = np.full((1, V), -np.inf, np.float32)
+    words = [10, 4000, 4001, 8000]
+    x[0, words], x[0, V - 1] = at, 0.0
+    x[0, 8192 + 5] = 1.0
+    w = np.exp(at - 1.0)  # (fp64; half a weight is far more than what it is off by)
+    total = 1.0 + np.exp(-1.0)
+    u = np.array([[0.5, 1.5, 2.5, 3.5, 4.5]]) * (w / total)
+    word, logp = _outs(1, 5)
+    sp.spdp_draw(state.h, dev(x), word, logp, work_for(1, V), u=dev(u))
+    assert word[0].tolist() == words + [8192 + 5]
+    want = np.array([at - 1.0] * 4 + [0.0]) - np.log(total)
+    np.testing.assert_allclose(logp[0].cpu().numpy(), want, rtol=2.0 ** -23)
