@@ -1281,3 +1281,132 @@ def test_draw_among_the_least_weights(state, at):
     assert word[0].tolist() == words + [8192 + 5]
     want = np.array([at - 1.0] * 4 + [0.0]) - np.log(total)
     np.testing.assert_allclose(logp[0].cpu().numpy(), want, rtol=2.0 ** -23)
+
+
+def _hard_rows(rng, rows, V):
+    """Rows that make choosing hard: ties at every height, rising and falling ones, a few words
+    left here and there, runs without any, lone peaks, wide ranges."""
+    x = rng.normal(size=(rows, V)).astype(np.float32) * 3
+    for i in range(rows):
+        kind = i % 9
+        if kind == 0:
+            x[i] = np.round(x[i])
+        elif kind == 1:
+            x[i] = np.arange(V) / 64.0
+        elif kind == 2:
+            x[i] = -np.arange(V) / 64.0
+        elif kind == 3:
+            x[i] = np.where(rng.random(V) < rng.choice([1e-3, 1e-2, 0.1]), x[i], -np.inf)
+        elif kind == 4:
+            for _ in range(6):
+                a = rng.integers(0, V)
+                x[i, a:a + rng.integers(1, max(2, V // 4))] = -np.inf
+        elif kind == 5:
+            x[i] = 2.0
+            x[i, rng.integers(0, V, 3)] = 1.0
+        elif kind == 6:
+            x[i] = -np.inf
+            a = rng.integers(0, max(1, V - 300))
+            x[i, a:a + 300] = -1.0
+        elif kind == 7:
+            x[i] *= 60
+        else:
+            x[i, : V // 2] = -50.0
+            x[i, rng.integers(0, V, 5)] = 40.0
+    return x
+
+
+def _best(x, k):
+    """As ow.top, for many words."""
+    order = np.lexsort((np.broadcast_to(np.arange(x.shape[1]), x.shape), -x), axis=1)[:, :k]
+    value = np.full((len(x), k), -np.inf, np.float32)
+    word = np.full((len(x), k), -1, np.int32)
+    value[:, :order.shape[1]] = np.take_along_axis(x, order, 1)
+    word[:, :order.shape[1]] = np.where(value[:, :order.shape[1]] > -np.inf, order, -1)
+    return word, value
+
+
+@pytest.mark.parametrize("rows,V", [(1100, 9000), (300, 20000), (18, 50000), (1030, 4100)])
+@pytest.mark.parametrize("k", [1, 10, 256])
+def test_top_of_hard_rows(state, rows, V, k):
+    """Parts of one and of several chunks, with and without rules."""
+    say(f"top {k} of {rows} x {V}, hard rows")
+    rng = np.random.default_rng(V + k)
+    x = _hard_rows(rng, rows, V)
+    some = np.unique(np.r_[0:min(rows, 45), rows - 18:rows])
+    r = RuleSet(rng, rows, V)
+    for rules, want in ((None, x[some]), (r, None)):
+        word, value = _outs(rows, k)
+        sp.spdp_top(state.h, dev(x), word, value, work_for(rows, V, k), rules=rules and rules.c)
+        if want is None:
+            o = {n: (np.asarray(t)[some] if n != "listed" else [t[i] for i in some])
+                 for n, t in r.o.items()}
+            want = ow.adjusted(x[some], **o)
+        ww, wv = _best(want, k)
+        np.testing.assert_array_equal(word[dev(some)].cpu().numpy(), ww)
+        np.testing.assert_array_equal(value[dev(some)].cpu().numpy(), wv)
+
+
+@pytest.mark.parametrize("rows,V,n", [(27, 5000, 70), (18, 9000, 70), (9, 100000, 20), (300, 6000, 500)])
+def test_draw_of_hard_rows(state, rows, V, n):
+    say(f"draw {n} of {rows} x {V}, hard rows")
+    rng = np.random.default_rng(V + n)
+    x = _hard_rows(rng, rows, V)
+    u = rng.random((rows, n))
+    some = np.unique(np.r_[0:min(rows, 9), rows - 9:rows])
+    r = RuleSet(rng, rows, V)
+    for rules, temperature in ((None, 1.0), (r, 0.5)):
+        word, logp = _outs(rows, n)
+        sp.spdp_draw(state.h, dev(x), word, logp, work_for(rows, V), u=dev(u), temperature=temperature,
+                     rules=rules and rules.c)
+        want = x[some]
+        if rules:
+            o = {m: (np.asarray(t)[some] if m != "listed" else [t[i] for i in some])
+                 for m, t in r.o.items()}
+            want = ow.adjusted(x[some], **o)
+        _check_draws(word[dev(some)].cpu().numpy(), logp[dev(some)].cpu().numpy(), want, u[some],
+                     temperature)
+
+
+def test_pack_of_blocks_without_numbers(state):
+    say("pack: blocks of NaN and infinities only")
+    rng = np.random.default_rng(5)
+    x = rng.normal(size=(6, 400))
+    x[0, :128], x[1, 128:256], x[2, 384:], x[3], x[4, ::2] = np.nan, np.inf, -np.inf, np.nan, np.inf
+    for t in ("f64", "f32"):
+        out = sp.spdp_pack8(state.h, dev(x, TYPES[t]), sp.Rows8.empty(6, 400))
+        q, e = ow.pack8(dev(x, TYPES[t]).double().cpu().numpy())
+        np.testing.assert_array_equal(out.e.cpu().numpy(), e)
+        np.testing.assert_array_equal(ow.value8(out.q.view(torch.uint8).cpu().numpy()), ow.value8(q))
+
+
+@pytest.mark.parametrize("m,n", [(17, 300), (300, 20000), (777, 10000), (1000, 14724)])
+def test_product_keeps_rows_apart(state, m, n):
+    """NaN, zeros and negative values of one document or word are seen in its own scores only."""
+    say(f"product {m} x {n}: rows apart")
+    (a8, _), (b8, _) = _model8(state, 3, m, n, 300)
+    out = sp.spdp_product8(state.h, a8, b8, torch.empty((m, n), device="cuda"), log=True)
+    assert torch.isfinite(out).all()
+    docs, words = [0, m // 2, m - 1], [0, 63, 64, n // 2, n - 65, n - 1]
+    a, b = a8.q.view(torch.uint8), b8.q.view(torch.uint8)
+    a[docs[0], 299] = 127
+    a[docs[1]] = 0
+    a[docs[2]] |= 128
+    b[words[0], 0] = 255
+    b[words[1]] = 0
+    b[words[2]] |= 128
+    b[words[3], 150] = 127
+    b[words[4]] |= 128
+    b[words[5]] = 0
+    got = sp.spdp_product8(state.h, a8, b8, torch.empty((m, n), device="cuda"), log=True)
+    keep_d, keep_w = torch.ones(m, dtype=torch.bool), torch.ones(n, dtype=torch.bool)
+    keep_d[docs], keep_w[words] = False, False
+    assert torch.equal(got[keep_d.cuda()][:, keep_w.cuda()], out[keep_d.cuda()][:, keep_w.cuda()])
+    w = keep_w.cuda()
+    assert torch.isnan(got[docs[0]]).all()
+    assert torch.isneginf(got[docs[1]][w]).all() and torch.isnan(got[docs[2]][w]).all()
+    d = keep_d.cuda()
+    nan, zero = [words[i] for i in (0, 2, 3, 4)], [words[i] for i in (1, 5)]
+    assert torch.isnan(got[d][:, nan]).all() and torch.isneginf(got[d][:, zero]).all()
+    # negative documents and words make positive sums
+    assert torch.equal(got[docs[2]][[words[2], words[4]]], out[docs[2]][[words[2], words[4]]])
