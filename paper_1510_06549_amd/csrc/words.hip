@@ -963,7 +963,7 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
 // One workgroup per (row, chunk): its largest score and its sums.  From rows of one chunk the
 // workgroup draws at once (ONE).
 //
-// 500 x 100 000 in bf16 (100 MB): 52 us, 65 with rules.  The scores' bytes would take 22:
+// 500 x 100 000 in bf16 (100 MB): 53 us, 65 with rules.  The scores' bytes would take 22:
 // what bounds it are 30 vector instructions for each score, 13 of them in fp64, which issue
 // without a pause for 41 us.
 template <typename T, bool ONE>
@@ -1049,7 +1049,7 @@ __global__ void __launch_bounds__(kDrawThreads, ONE ? 4 : 8) k_draw_parts(
 }
 
 // `share` workgroups of four wavefronts per row, `each` draws a wavefront.  250 draws of each
-// of 500 rows: 27 us, 38 with rules, mostly in wait of the sums and scores that the draws
+// of 500 rows: 28 us, 38 with rules, mostly in wait of the sums and scores that the draws
 // land on (16 us of instructions).
 template <typename T>
 __global__ void __launch_bounds__(256) k_draw(const T *__restrict__ x, int64_t ld, int64_t V,
