@@ -857,11 +857,13 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
         // A word has weight where it is above 2^-1075 beside the row's largest, which fp64 rounds to
         // 0: beside its chunk's largest, above `least` (0 where that is the row's).
         double least = 0.0;
-        if (chunks > 1 && __any(!(goal > 0.0))) {
+        int way = 0;  // from where the first (1) or last (-1) such word is looked for, if by itself
+        if (chunks > 1 && __any(lane < many && !(goal > 0.0))) {
             least = power_of(-1075.0 * kPowers - (own - law.top) * scale, powers);
+            if (lane < many && least > 0.0) way = end ? -1 : !(goal > 0.0) ? 1 : 0;
             if (!end) goal = fmax(goal, least);
         }
-        const bool ends = chunks > 1 && __any(end && least > 0.0);
+        const bool ends = chunks > 1 && __any(way != 0);
         // the block (four draws' sums requested at a time)
         int32_t block = 0;
         for (int32_t t4 = 0; t4 < many; t4 += 4) {
@@ -943,12 +945,29 @@ __device__ __forceinline__ void draw_words(const T *__restrict__ x, int64_t V, c
                 const double weight = weight_of(s, top, scale, powers);
                 const double upto = row_prefix(weight);
                 const u64 positive = __ballot(weight > 0.0), past = __ballot(upto > g) & positive;
-                const uint32_t in_row = (uint32_t)(past >> (lane & 48)) & 0xFFFFu;
+                uint32_t in_row = (uint32_t)(past >> (lane & 48)) & 0xFFFFu;
                 uint32_t have = (uint32_t)(positive >> (lane & 48)) & 0xFFFFu;
-                if (ends) {  // (a goal past all: the last with weight beside the row's largest)
-                    const u64 above = __ballot(weight > __shfl(least, t));
-                    const uint32_t its = (uint32_t)(above >> (lane & 48)) & 0xFFFFu;
-                    have = its && !(g < __builtin_inf()) ? its : have;
+                if (ends) {
+                    // quarter by quarter, whose sums say only that their words together may have
+                    // weight, until a word has, the chunk's largest at the latest
+                    const double floor = __shfl(least, t);
+                    const int by = __shfl(way, t);
+                    double at_base = weight;
+                    uint32_t its = 0;
+                    for (int left = kQuarters; left > 0; --left) {
+                        const u64 above = __ballot(at_base > floor);
+                        its = (uint32_t)(above >> (lane & 48)) & 0xFFFFu;
+                        const bool more = by != 0 && its == 0;
+                        if (!__any(more)) break;
+                        if (more) base[j] += by * kQuarterWords;
+                        const int64_t w = (int64_t)base[j] + place;
+                        s = -__builtin_inff();
+                        const int n = r.n_words > 0 ? times(base[j]) : 0;
+                        if (w >= 0 && w < V) s = ruled(r, (float)x[w], w, n);
+                        at_base = weight_of(s, top, scale, powers);
+                    }
+                    in_row = by == 0 ? in_row : by > 0 ? its : 0;
+                    have = by < 0 ? its : have;
                 }
                 const int l = in_row ? __builtin_ctz(in_row) : 31 - __builtin_clz(have | 1u);
                 if (place == l && t < many) {

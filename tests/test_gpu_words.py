@@ -1410,3 +1410,37 @@ def test_product_keeps_rows_apart(state, m, n):
     assert torch.isnan(got[d][:, nan]).all() and torch.isneginf(got[d][:, zero]).all()
     # negative documents and words make positive sums
     assert torch.equal(got[docs[2]][[words[2], words[4]]], out[docs[2]][[words[2], words[4]]])
+
+
+@pytest.mark.parametrize("V,step,temperature", [(20000, 1 / 64, 0.05), (20000, -1 / 64, 0.05),
+                                                (30000, 1 / 256, 0.01), (9000, -0.5, 1.0),
+                                                (9000, 0.5, 1.0), (700000, 2.0 ** -13, 2.0 ** -6)])
+def test_draw_ends_of_slopes(state, V, step, temperature):
+    """Rows that rise or fall: around the first and the last word with weight stand many that
+    have some together and none each."""
+    say(f"draw: ends of a slope of {step} over {V} words at {temperature}")
+    x = np.stack([np.arange(V) * step, np.arange(V) * step + 0.3 * np.sin(np.arange(V))]).astype(np.float32)
+    u = np.tile(np.array([0.0, 1.0, 0.5] * 30 + [-1.0, 2.0]), (2, 1))
+    rng = np.random.default_rng(V)
+    words = rng.integers(0, V, 4000)
+    r = sp.Rules(2, V, doc_off=dev(np.array([0, 1000, 4000])), words=dev(words.astype(np.int32)),
+                 penalties=dev(np.tile(np.array([1.0, 0.5 * abs(step), 0.0], np.float32), (2, 1))))
+    for rules in (None, r):
+        xo = x if rules is None else ow.adjusted(x, [words[:1000], words[1000:]],
+                                                 [[1.0, 0.5 * abs(step), 0.0]] * 2)
+        word, logp = _outs(2, 92)
+        sp.spdp_draw(state.h, dev(x), word, logp, work_for(2, V), u=dev(u), rules=rules,
+                     temperature=temperature)
+        with np.errstate(under="ignore"):
+            z = (xo.astype(np.float64) - xo.max(1, keepdims=True).astype(np.float64)) / temperature
+            law = np.exp(z)
+        for i in range(2):
+            # (words whose weight lies at the border of what fp64 rounds to 0 are as good as those
+            # next to them: the logarithm of 2^-1075 to 1e-9)
+            sure, any_ = z[i] > -1075 * np.log(2) + 1e-9, z[i] > -1075 * np.log(2) - 1e-9
+            got = word[i].cpu().numpy()
+            for t, of in ((0, 0), (1, -1)):
+                ends = {int(np.flatnonzero(m)[of]) for m in (sure, any_)}
+                assert set(got[t:90:3].tolist()) | {int(got[90 + t])} <= ends, (i, t, ends, got[t])
+            c = np.cumsum(law[i].astype(np.longdouble))
+            assert (got[2:90:3] == np.searchsorted(c, 0.5 * c[-1], side="right")).all()
